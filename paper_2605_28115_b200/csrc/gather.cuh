@@ -16,6 +16,7 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
+#include "index_check.cuh"
 #include "pdl.cuh"
 
 namespace civic {
@@ -47,19 +48,6 @@ struct GatherParams {
     int32_t* check;
     int32_t n_pages;
 };
-
-// Fault record of the checked kernels: {code, plane, position, offending value}.  The first
-// thread to find a fault claims word 0 (0 -> code) and fills in the rest; later faults leave the
-// record alone, so it names ONE offending entry.  The record is sticky: only the caller clears it.
-enum IndexFault { kIndexOk = 0, kIndexOutOfRange = 1, kIndexNotAscending = 2, kIndexBadPage = 3 };
-__device__ __forceinline__ void report_bad_index(int32_t* record, int code, int plane, int pos, int value)
-{
-    if (atomicCAS(record, 0, code) == 0) {
-        record[1] = plane;
-        record[2] = pos;
-        record[3] = value;
-    }
-}
 
 template <typename VecT>
 __device__ __forceinline__ VecT load_stream(const VecT* p);
