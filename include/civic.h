@@ -443,6 +443,142 @@ civic_status_t civic_kv_compressed_attention_prepared(const void* q, const void*
                                                       int32_t* device_status, void* stream);
 
 /*
+ * The quantised K/V cache: kept rows in 4 or 8 bits, and attention over them.
+ *
+ * Paper: the cache storage term of Eq. 2 / Eq. 7 and the ratio of Eq. 14 count kept rows; these calls
+ * shrink what a kept row occupies and let the decoder read it as it lies.  The paper has no
+ * counterpart to the number format.
+ *
+ * Format.  A group is 32 consecutive channels of one token's K (or V) row of one head.  With
+ * L = 2^bits - 1 a group is held as its minimum m, a scale s and 32 codes:
+ *     s = (max - m) / L rounded up to the payload type,  code = floor((x - m) / s + 1/2)
+ * and stands for s * code + m, so that no value is off by more than s / 2.  A group with a NaN, an
+ * infinity or a range beyond fp32 stands for 32 NaN.  In bf16 a range below L * 2^-126 counts as 0.
+ * A row of one head takes head_dim * bits / 8 + head_dim / 32 * 4 bytes (head_dim 128: 80 in 4 bits
+ * and 144 in 8 bits instead of 256).
+ *
+ * Layout.  A layer's cache is [n_pages, n_heads, page_size / 16] tiles of 16 tokens; a tile holds
+ * K codes, V codes, K parameters, V parameters ({s, m} for [16 tokens][groups]), codes in 32-bit words:
+ *   K  word w of lane t (0 .. 3) of a row holds, lowest bits first, consecutive channels from
+ *      32 j + 8 t (+ 4 for the second word in 8 bits) on; w = j in 4 bits, 2 j and 2 j + 1 in 8 bits.  With
+ *      W = head_dim / 32 * bits / 4 words and P = min(4, W):  [W / P][16 rows][4 lanes][P words].
+ *   V  word w of lane (g, t), g < 8, t < 4, of half h holds consecutive channels from 32 j + 4 g (+ 2 for
+ *      the second word in 8 bits) on: of token 8 h + 2 t in its low, of token 8 h + 2 t + 1 in its high
+ *      16 bits:  [2 halves][W / P][32 lanes 4 g + t][P words].
+ *
+ * head_dim 64, 128 or 256; bits 4 or 8; page_size a multiple of 16 up to 1024; up to 1024 heads;
+ * dtype the 16-bit type of the rows, of q and out, and of the parameters: CIVIC_ERR_UNSUPPORTED
+ * otherwise.  Pointers to rows and caches 16-byte aligned, strides multiples of 8 elements.
+ *
+ * Pages.  Token i of sequence s lives in page block_table[s, i / page_size].  Entries a call does not
+ * need may hold anything.  A page outside [0, n_pages), or a token behind the table's last entry, is
+ * neither read nor written (attention leaves its tokens out); with civic_set_index_check the fault is
+ * recorded as CIVIC_INDEX_BAD_PAGE.  Sequences that write must own distinct pages.
+ */
+typedef enum { CIVIC_BF16 = 0, CIVIC_FP16 = 1 } civic_dtype_t;
+
+typedef struct {
+    int32_t n_pages, page_size, n_heads, head_dim; /* one layer's cache; n_heads = K/V heads       */
+    int32_t bits;                                  /* 4 or 8                                        */
+    int32_t dtype;                                 /* civic_dtype_t                                 */
+} civic_quant_desc_t;
+
+/* Strides of a [n_seq, rows, heads, head_dim] tensor of 16-bit elements, in elements; the last
+ * dimension is contiguous.  Token-major, head-major and slices of a fused projection all fit. */
+typedef struct {
+    int64_t seq, token, head;
+} civic_row_strides_t;
+
+/* Bytes of one page (all heads) of one layer; 0 if the description is invalid or unsupported. */
+size_t civic_quant_page_bytes(const civic_quant_desc_t* desc);
+
+/*
+ * civic_compact_kv_quant -- civic_compact_kv_paged into a quantised cache: every layer's kept K and V
+ * rows are gathered, quantised and stored in ONE launch per 80 layers.
+ *
+ * Paper: as civic_compact_kv_paged.  Row seq_idx[s, j] of k_src[l] / v_src[l] becomes token j of
+ * sequence s in cache[l].
+ *
+ * k_src, v_src  host arrays of n_layers dev pointers, tensors [n_seq, seq_len, n_heads, head_dim] with
+ *               src_strides (host)
+ * seq_idx       dev [n_seq, s_out] int32, values in [0, seq_len); others are neither read nor written
+ *               (CIVIC_INDEX_OUT_OF_RANGE with civic_set_index_check)
+ * cache         host array of n_layers dev pointers, each n_pages * civic_quant_page_bytes(desc) bytes
+ * block_table   dev [n_seq, max_pages_per_seq] int32; max_pages_per_seq * page_size < s_out is
+ *               CIVIC_ERR_INVALID_ARG
+ */
+civic_status_t civic_compact_kv_quant(const void* const* k_src, const void* const* v_src, const civic_row_strides_t* src_strides,
+                                      int32_t n_layers, int32_t n_seq, int32_t seq_len, int32_t s_out, const int32_t* seq_idx,
+                                      void* const* cache, const civic_quant_desc_t* desc, const int32_t* block_table,
+                                      int32_t max_pages_per_seq, void* stream);
+
+/*
+ * civic_append_kv_quant -- new tokens' K and V rows into the quantised cache (a decode step, a later
+ * prompt).  Paper: no counterpart; the cache of Eq. 14 grows by one row per generated token.
+ *
+ * Row j < counts[s] of sequence s becomes token start[s] + j; the other tokens of the tiles it falls
+ * into are left as they were.
+ *
+ * k_new, v_new  host arrays of n_layers dev pointers, tensors [n_seq, n_new, n_heads, head_dim]
+ * start         dev [n_seq] int32, >= 0: tokens the sequence holds already
+ * counts        dev [n_seq] int32 or NULL = n_new for every sequence (values beyond n_new count as n_new,
+ *               below 0 as 0)
+ */
+civic_status_t civic_append_kv_quant(const void* const* k_new, const void* const* v_new, const civic_row_strides_t* src_strides,
+                                     int32_t n_layers, int32_t n_seq, int32_t n_new, const int32_t* start, const int32_t* counts,
+                                     void* const* cache, const civic_quant_desc_t* desc, const int32_t* block_table,
+                                     int32_t max_pages_per_seq, void* stream);
+
+/*
+ * civic_read_kv_quant -- rows of the quantised cache as dense tensors, s * code + m rounded to the
+ * payload type.  Paper: no counterpart.
+ *
+ * Token start[s] + j (start NULL: j) of sequence s becomes row j < counts[s] of k_dst[l] / v_dst[l];
+ * the rows from counts[s] on are left as they were.
+ *
+ * counts        dev [n_seq] int32 (values beyond max_rows count as max_rows, below 0 as 0)
+ * k_dst, v_dst  host arrays of n_layers dev pointers, tensors [n_seq, max_rows, n_heads, head_dim] with
+ *               dst_strides (host), under which no two elements may share a place; K and V may be
+ *               slices of one buffer
+ */
+civic_status_t civic_read_kv_quant(const void* const* cache, const civic_quant_desc_t* desc, const int32_t* block_table,
+                                   int32_t max_pages_per_seq, int32_t n_layers, int32_t n_seq, int32_t max_rows,
+                                   const int32_t* start, const int32_t* counts, void* const* k_dst, void* const* v_dst,
+                                   const civic_row_strides_t* dst_strides, void* stream);
+
+/*
+ * civic_quant_attention -- attention of query tokens over one layer's quantised cache.
+ *
+ * Paper: the decoder's attention over the compact cache (Section 3.5; Eq. 2's attention term), which
+ * the paper leaves to the serving engine.  Query head h reads K/V head h / (q_heads / n_heads):
+ *     S_j = scale * q . k_j,   out = sum_j exp(S_j - lse) v_j,   lse = log sum_j exp(S_j)
+ * over the tokens j < lens[s], with `causal` only j < lens[s] - q_lens[s] + i + 1 for query token i:
+ * the query tokens are the sequence's last ones and are in the cache already.  A query row that sees
+ * no token gets out = 0 and lse = -infinity.
+ *
+ * q           dev [n_seq, q_len, q_heads, head_dim] with q_strides (host)
+ * cache       dev, one layer
+ * lens        dev [n_seq] int32, tokens in the cache; 0 for an empty slot of a padded batch (below 0
+ *             counts as 0, beyond max_pages_per_seq * page_size as that)
+ * q_lens      dev [n_seq] int32 or NULL = q_len: query tokens of each sequence; out and lse rows behind
+ *             them are left as they were
+ * out         dev [n_seq, q_len, q_heads, head_dim] contiguous, written
+ * lse         dev fp32 [n_seq, q_len, q_heads] or NULL, written; natural logarithm
+ * workspace   dev scratch of civic_quant_attention_workspace_bytes(...) bytes, 256-byte aligned; contents
+ *             on entry are irrelevant.  Calls that may overlap on the GPU need separate workspaces
+ * Weights and codes are multiplied as fp16 with fp32 accumulation, scores, sums and lse are fp32.  V
+ * groups' scales are expected within 2^-86 .. 2^89, scores may have any size.  Two launches.
+ */
+civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q_strides, const void* cache,
+                                     const civic_quant_desc_t* desc, const int32_t* block_table, int32_t max_pages_per_seq,
+                                     const int32_t* lens, const int32_t* q_lens, int32_t n_seq, int32_t q_len, int32_t q_heads,
+                                     float scale, int32_t causal, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/* Scratch bytes civic_quant_attention needs; 0 if the shape is invalid or unsupported. */
+size_t civic_quant_attention_workspace_bytes(const civic_quant_desc_t* desc, int32_t n_seq, int32_t q_len, int32_t q_heads);
+
+/*
  * Device-side validation of index arrays.
  *
  * Paper: the compact rows are "indexed by compact visual segments" with inherited positions

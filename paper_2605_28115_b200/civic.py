@@ -34,7 +34,9 @@ EXPORTS = ("civic_select", "civic_select_max_tokens", "civic_reserved_count", "c
            "civic_kv_compressed_attention", "civic_kv_compressed_attention_workspace_bytes",
            "civic_set_index_check", "civic_validate_indices", "civic_selftest_bounded_wait",
            "civic_anchor_prepared_bytes", "civic_anchor_prepare", "civic_anchor_aggregate_prepared",
-           "civic_kv_attention_prepared_bytes", "civic_kv_attention_prepare", "civic_kv_compressed_attention_prepared")
+           "civic_kv_attention_prepared_bytes", "civic_kv_attention_prepare", "civic_kv_compressed_attention_prepared",
+           "civic_quant_page_bytes", "civic_compact_kv_quant", "civic_append_kv_quant", "civic_read_kv_quant",
+           "civic_quant_attention", "civic_quant_attention_workspace_bytes")
 
 INDEX_FAULTS = ("CIVIC_INDEX_OK", "CIVIC_INDEX_OUT_OF_RANGE", "CIVIC_INDEX_NOT_ASCENDING", "CIVIC_INDEX_BAD_PAGE")
 
@@ -51,6 +53,17 @@ class SelectDesc(ctypes.Structure):
     _fields_ = [("t", ctypes.c_int32), ("h", ctypes.c_int32), ("w", ctypes.c_int32),
                 ("region_h", ctypes.c_int32), ("region_w", ctypes.c_int32),
                 ("floor_per_region", ctypes.c_int32), ("k", ctypes.c_int32)]
+
+
+class QuantDesc(ctypes.Structure):
+    """civic_quant_desc_t"""
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("bits", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class RowStrides(ctypes.Structure):
+    """civic_row_strides_t"""
+    _fields_ = [("seq", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -137,6 +150,20 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.civic_validate_indices.restype = ctypes.c_int
     lib.civic_selftest_bounded_wait.argtypes = [ctypes.c_uint64, vp, vp]
     lib.civic_selftest_bounded_wait.restype = ctypes.c_int
+    desc, strides = ctypes.POINTER(QuantDesc), ctypes.POINTER(RowStrides)
+    lib.civic_quant_page_bytes.argtypes = [desc]
+    lib.civic_quant_page_bytes.restype = sz
+    lib.civic_compact_kv_quant.argtypes = [vpp, vpp, strides, i32, i32, i32, i32, vp, vpp, desc, vp, i32, vp]
+    lib.civic_compact_kv_quant.restype = ctypes.c_int
+    lib.civic_append_kv_quant.argtypes = [vpp, vpp, strides, i32, i32, i32, vp, vp, vpp, desc, vp, i32, vp]
+    lib.civic_append_kv_quant.restype = ctypes.c_int
+    lib.civic_read_kv_quant.argtypes = [vpp, desc, vp, i32, i32, i32, i32, vp, vp, vpp, vpp, strides, vp]
+    lib.civic_read_kv_quant.restype = ctypes.c_int
+    lib.civic_quant_attention.argtypes = [vp, strides, vp, desc, vp, i32, vp, vp, i32, i32, i32, ctypes.c_float, i32, vp, vp,
+                                          vp, sz, vp]
+    lib.civic_quant_attention.restype = ctypes.c_int
+    lib.civic_quant_attention_workspace_bytes.argtypes = [desc, i32, i32, i32]
+    lib.civic_quant_attention_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -732,6 +759,207 @@ def civic_kv_compressed_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Ten
     with _on_device(dev):
         _check(fn(*args, _stream_ptr(stream)), "civic_kv_compressed_attention")
     return out, device_status
+
+
+QUANT_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+QUANT_TILE = 16   # tokens per tile of the quantised cache
+QUANT_GROUP = 32  # channels per scale
+
+
+def quant_tile_bytes(head_dim: int, bits: int) -> int:
+    """Bytes of 16 tokens' K and V of one head in the quantised cache."""
+    return 2 * (QUANT_TILE * head_dim * bits // 8 + QUANT_TILE * (head_dim // QUANT_GROUP) * 4)
+
+
+class QuantCache:
+    """A quantised paged K/V cache over `buffer`, uint8 [n_layers, n_pages, n_heads, page bytes] (contiguous,
+    caller-owned; the format is civic.h's).  `dtype` (bfloat16 or float16) is the type of the rows, of the
+    queries and of the outputs."""
+
+    __slots__ = ("buffer", "page_size", "head_dim", "bits", "dtype", "n_layers", "n_pages", "n_heads", "desc", "ptr",
+                 "layer_bytes")
+
+    def __init__(self, buffer: torch.Tensor, page_size: int, head_dim: int, bits: int, dtype: torch.dtype = torch.bfloat16):
+        if dtype not in QUANT_DTYPES:
+            raise ValueError("dtype must be torch.bfloat16 or torch.float16")
+        if buffer.dim() != 4:
+            raise ValueError("buffer must be [n_layers, n_pages, n_heads, page bytes]")
+        if not buffer.is_cuda:
+            raise ValueError("buffer must be a CUDA tensor")
+        self.ptr = _dev_ptr(buffer, "buffer", torch.uint8)
+        self.n_layers, self.n_pages, self.n_heads, per_head = buffer.shape
+        self.desc = QuantDesc(self.n_pages, page_size, self.n_heads, head_dim, bits, QUANT_DTYPES[dtype])
+        self.layer_bytes = self.n_pages * int(load().civic_quant_page_bytes(ctypes.byref(self.desc)))
+        if self.layer_bytes == 0:
+            raise CivicError(5, "QuantCache")
+        if self.layer_bytes != self.n_pages * self.n_heads * per_head:
+            raise ValueError("buffer's last dimension must be page_size / 16 * quant_tile_bytes(head_dim, bits)")
+        self.buffer, self.page_size, self.head_dim, self.bits, self.dtype = buffer, page_size, head_dim, bits, dtype
+
+    def _table(self) -> ctypes.Array:
+        return (ctypes.c_void_p * self.n_layers)(*range(self.ptr, self.ptr + self.n_layers * self.layer_bytes,
+                                                        self.layer_bytes))
+
+
+def quant_cache(n_layers: int, n_pages: int, n_heads: int, head_dim: int, page_size: int = 16, bits: int = 4,
+                dtype: torch.dtype = torch.bfloat16, device="cuda") -> QuantCache:
+    """A new, unwritten QuantCache."""
+    if page_size < 1 or page_size % QUANT_TILE:
+        raise ValueError("page_size must be a multiple of 16")
+    buffer = torch.empty((n_layers, n_pages, n_heads, page_size // QUANT_TILE * quant_tile_bytes(head_dim, bits)),
+                         dtype=torch.uint8, device=device)
+    return QuantCache(buffer, page_size, head_dim, bits, dtype)
+
+
+def _rows_of(cache: QuantCache, x, what: str):
+    """Per-layer row tensors [n_seq, rows, n_heads, head_dim], stacked [n_layers, ...] or as a sequence ->
+    (pointer table, strides, n_seq, rows).  Any strides with a contiguous last dimension, the same for all layers."""
+    if isinstance(x, torch.Tensor):
+        if x.dim() != 5 or x.shape[0] != cache.n_layers:
+            raise ValueError(f"{what} must be [n_layers, n_seq, rows, n_heads, head_dim]")
+        _, n_seq, rows, heads, dim = x.shape
+        per_layer, seq, token, head, last = x.stride()
+        first, base, step = x, x.data_ptr(), per_layer * x.element_size()
+        table = (ctypes.c_void_p * cache.n_layers)(*[base + i * step for i in range(cache.n_layers)])
+    else:
+        if len(x) != cache.n_layers or any(t.dim() != 4 for t in x):
+            raise ValueError(f"{what} must be one [n_seq, rows, n_heads, head_dim] tensor per layer of the cache")
+        first = x[0]
+        if any(t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype or t.device != first.device
+               for t in x):
+            raise ValueError(f"all {what} tensors must share shape, strides, dtype and device")
+        n_seq, rows, heads, dim = first.shape
+        seq, token, head, last = first.stride()
+        table = (ctypes.c_void_p * cache.n_layers)(*[t.data_ptr() for t in x])
+    if heads != cache.n_heads or dim != cache.head_dim or first.dtype != cache.dtype:
+        raise ValueError(f"{what} must have the cache's {cache.n_heads} heads of {cache.head_dim} in {cache.dtype}")
+    if last != 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+    _on_cache_device(cache, first, what)
+    return table, (seq, token, head), n_seq, rows
+
+
+def _on_cache_device(cache: QuantCache, x: torch.Tensor, what: str) -> None:
+    if not (x.device == cache.buffer.device or x.is_pinned()):
+        raise ValueError(f"{what} must be on the cache's device {cache.buffer.device}")
+
+
+def _seq_words(cache: QuantCache, x: Optional[torch.Tensor], n_seq: int, what: str, dims: int = 1) -> Optional[int]:
+    """Pointer of an int32 tensor whose first dimension is n_seq."""
+    if x is None:
+        return None
+    if x.dim() != dims or x.shape[0] != n_seq:
+        raise ValueError(f"{what} must be [n_seq]" if dims == 1 else f"{what} must be [n_seq, ...]")
+    _on_cache_device(cache, x, what)
+    return _dev_ptr(x, what, torch.int32)
+
+
+def civic_compact_kv_quant(k_src, v_src, seq_idx: torch.Tensor, cache: QuantCache, block_table: torch.Tensor,
+                           stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Kept rows of every layer's K and V, quantised, into `cache`: row seq_idx[s, j] becomes token j of sequence s.
+    k_src, v_src [n_layers, n_seq, seq_len, n_heads, head_dim] (or a sequence of per-layer tensors) with equal
+    strides; seq_idx int32 [n_seq, s_out]; block_table int32 [n_seq, max_pages_per_seq]."""
+    k, strides, n_seq, seq_len = _rows_of(cache, k_src, "k_src")
+    v, v_strides, *v_shape = _rows_of(cache, v_src, "v_src")
+    if v_strides != strides or v_shape != [n_seq, seq_len]:
+        raise ValueError("k_src and v_src must share shape and strides")
+    idx = _seq_words(cache, seq_idx, n_seq, "seq_idx", 2)
+    table = _seq_words(cache, block_table, n_seq, "block_table", 2)
+    with _on_device(cache.buffer.device):
+        _check(load().civic_compact_kv_quant(k, v, ctypes.byref(RowStrides(*strides)), cache.n_layers, n_seq, seq_len,
+                                             seq_idx.shape[1], idx, cache._table(), ctypes.byref(cache.desc), table,
+                                             block_table.shape[1], _stream_ptr(stream)), "civic_compact_kv_quant")
+
+
+def civic_append_kv_quant(k_new, v_new, start: torch.Tensor, cache: QuantCache, block_table: torch.Tensor,
+                          counts: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """New tokens' rows into `cache`: row j < counts[s] (default: all) becomes token start[s] + j of sequence s.
+    k_new, v_new [n_layers, n_seq, n_new, n_heads, head_dim] (or a sequence of per-layer tensors); start, counts
+    int32 [n_seq]; block_table int32 [n_seq, max_pages_per_seq]."""
+    k, strides, n_seq, n_new = _rows_of(cache, k_new, "k_new")
+    v, v_strides, *v_shape = _rows_of(cache, v_new, "v_new")
+    if v_strides != strides or v_shape != [n_seq, n_new]:
+        raise ValueError("k_new and v_new must share shape and strides")
+    at = _seq_words(cache, start, n_seq, "start")
+    some = _seq_words(cache, counts, n_seq, "counts")
+    table = _seq_words(cache, block_table, n_seq, "block_table", 2)
+    with _on_device(cache.buffer.device):
+        _check(load().civic_append_kv_quant(k, v, ctypes.byref(RowStrides(*strides)), cache.n_layers, n_seq, n_new, at, some,
+                                            cache._table(), ctypes.byref(cache.desc), table, block_table.shape[1],
+                                            _stream_ptr(stream)), "civic_append_kv_quant")
+
+
+def civic_read_kv_quant(cache: QuantCache, block_table: torch.Tensor, counts: torch.Tensor, k_out, v_out,
+                        start: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Rows of `cache` in its dtype: token start[s] + j (start None: j) of sequence s to row j < counts[s] of k_out and
+    v_out [n_layers, n_seq, max_rows, n_heads, head_dim] (or sequences of per-layer tensors); the rows behind are
+    left as they were.  counts, start int32 [n_seq].  Returns (k_out, v_out)."""
+    k, strides, n_seq, rows = _rows_of(cache, k_out, "k_out")
+    v, v_strides, *v_shape = _rows_of(cache, v_out, "v_out")
+    if v_strides != strides or v_shape != [n_seq, rows]:
+        raise ValueError("k_out and v_out must share shape and strides")
+    some = _seq_words(cache, counts, n_seq, "counts")
+    at = _seq_words(cache, start, n_seq, "start")
+    table = _seq_words(cache, block_table, n_seq, "block_table", 2)
+    with _on_device(cache.buffer.device):
+        _check(load().civic_read_kv_quant(cache._table(), ctypes.byref(cache.desc), table, block_table.shape[1],
+                                          cache.n_layers, n_seq, rows, at, some, k, v, ctypes.byref(RowStrides(*strides)),
+                                          _stream_ptr(stream)), "civic_read_kv_quant")
+    return k_out, v_out
+
+
+def quant_attention_workspace_bytes(cache: QuantCache, n_seq: int, q_len: int, q_heads: int) -> int:
+    return int(load().civic_quant_attention_workspace_bytes(ctypes.byref(cache.desc), n_seq, q_len, q_heads))
+
+
+def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_table: torch.Tensor, lens: torch.Tensor,
+                          scale: Optional[float] = None, causal: bool = True, q_lens: Optional[torch.Tensor] = None,
+                          out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                          workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """softmax(scale q K^T) V over one layer of `cache` (scale default head_dim ** -0.5) ->
+    (out [n_seq, q_len, q_heads, head_dim], lse fp32 [n_seq, q_len, q_heads] or None).
+    q [n_seq, q_len, q_heads, head_dim], any strides with a contiguous last dimension; lens int32 [n_seq] tokens in the
+    cache, the query tokens among them (causal: they are the last ones); q_lens int32 [n_seq] query tokens of each
+    sequence (default: all q_len), rows behind them are left as they were."""
+    if q.dim() != 4 or q.shape[3] != cache.head_dim or q.dtype != cache.dtype or q.stride(3) != 1:
+        raise ValueError(f"q must be [n_seq, q_len, q_heads, {cache.head_dim}] in {cache.dtype}, its last dimension contiguous")
+    if not 0 <= layer < cache.n_layers:
+        raise ValueError("layer must be one of the cache's")
+    _on_cache_device(cache, q, "q")
+    n_seq, q_len, q_heads, dim = q.shape
+    dev = cache.buffer.device
+    table = _seq_words(cache, block_table, n_seq, "block_table", 2)
+    n_tok = _seq_words(cache, lens, n_seq, "lens")
+    n_q = _seq_words(cache, q_lens, n_seq, "q_lens")
+    made = []  # allocated here: not to be handed out again before `stream` is done with it
+    if out is None:
+        out = torch.empty((n_seq, q_len, q_heads, dim), dtype=cache.dtype, device=dev)
+        made.append(out)
+    elif tuple(out.shape) != (n_seq, q_len, q_heads, dim):
+        raise ValueError("out must have q's shape")
+    if lse is None and want_lse:
+        lse = torch.empty((n_seq, q_len, q_heads), dtype=torch.float32, device=dev)
+        made.append(lse)
+    elif lse is not None and tuple(lse.shape) != (n_seq, q_len, q_heads):
+        raise ValueError("lse must be [n_seq, q_len, q_heads]")
+    need = quant_attention_workspace_bytes(cache, n_seq, q_len, q_heads)
+    if workspace is None:
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        made.append(workspace)
+    else:
+        _on_cache_device(cache, workspace, "workspace")
+    seq, token, head, _ = q.stride()
+    if stream is not None:
+        for t in made:
+            t.record_stream(stream)
+    with _on_device(dev):
+        _check(load().civic_quant_attention(
+            q.data_ptr(), ctypes.byref(RowStrides(seq, token, head)), cache.ptr + layer * cache.layer_bytes,
+            ctypes.byref(cache.desc), table, block_table.shape[1], n_tok, n_q, n_seq, q_len, q_heads,
+            dim ** -0.5 if scale is None else scale, 1 if causal else 0, _dev_ptr(out, "out", cache.dtype),
+            _dev_ptr(lse, "lse", torch.float32), _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel(),
+            _stream_ptr(stream)), "civic_quant_attention")
+    return out, lse
 
 
 class index_check:

@@ -1,0 +1,388 @@
+// C ABI of the quantised K/V cache: host-side validation and launches of the kernels in
+// quant_cache.cuh and quant_attention.cuh.  See include/civic.h for the contract of every entry point.
+#include <cmath>
+#include <cstring>
+
+#include "host.hpp"
+#include "quant_attention.cuh"
+#include "quant_cache.cuh"
+
+using namespace civic_host;
+
+namespace {
+
+// CIVIC_OK, or why this description is none the kernels handle.
+civic_status_t check_desc(const civic_quant_desc_t* d)
+{
+    if (!d || d->n_pages < 1 || d->n_heads < 1 || d->page_size < 1 || d->head_dim < 1) return CIVIC_ERR_INVALID_ARG;
+    if (d->bits != 4 && d->bits != 8) return CIVIC_ERR_UNSUPPORTED;
+    if (d->dtype != CIVIC_BF16 && d->dtype != CIVIC_FP16) return CIVIC_ERR_UNSUPPORTED;
+    if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256) return CIVIC_ERR_UNSUPPORTED;
+    if (d->page_size % civic::kQuantTile || d->page_size > 1024 || d->n_heads > 1024) return CIVIC_ERR_UNSUPPORTED;
+    return CIVIC_OK;
+}
+
+size_t page_bytes(const civic_quant_desc_t& d)
+{
+    return (size_t)d.n_heads * (d.page_size / civic::kQuantTile) * civic::quant_tile_bytes(d.head_dim, d.bits);
+}
+
+// Bytes from a strided tensor's first element to behind its last.
+size_t extent_bytes(const civic_row_strides_t& s, int64_t n_seq, int64_t rows, int64_t heads, int64_t head_dim)
+{
+    return (size_t)((n_seq - 1) * s.seq + (rows - 1) * s.token + (heads - 1) * s.head + head_dim) * 2;
+}
+
+// Strides: multiples of 16 bytes, not negative; no overflow of the address arithmetic.
+civic_status_t check_strides(const civic_row_strides_t* s)
+{
+    if (!s || s->seq < 0 || s->token < 0 || s->head < 0) return CIVIC_ERR_INVALID_ARG;
+    if (s->seq % 8 || s->token % 8 || s->head % 8) return CIVIC_ERR_ALIGNMENT;
+    const int64_t limit = (int64_t)1 << 40;
+    if (s->seq > limit || s->token > limit || s->head > limit) return CIVIC_ERR_UNSUPPORTED;
+    return CIVIC_OK;
+}
+
+// Whether distinct (sequence, row, head) triples have distinct places: in ascending order of stride,
+// each stride at least spans what the smaller ones reach.
+bool writable_strides(const civic_row_strides_t& s, int64_t n_seq, int64_t rows, int64_t heads, int64_t head_dim)
+{
+    int64_t stride[3] = {s.seq, s.token, s.head}, n[3] = {n_seq, rows, heads}, reach = head_dim;
+    for (int pass = 0; pass < 3; ++pass) {
+        int best = -1;
+        for (int i = 0; i < 3; ++i)
+            if (n[i] > 1 && (best < 0 || stride[i] < stride[best])) best = i;
+        if (best < 0) break;
+        if (stride[best] < reach) return false;
+        reach += (n[best] - 1) * stride[best];
+        n[best] = 1;
+    }
+    return true;
+}
+
+// Whether the two lists of equal-sized ranges touch; one comparison of their hulls in the usual case.
+bool lists_overlap(const void* const* a, int na, size_t a_bytes, const void* const* b, int nb, size_t b_bytes)
+{
+    uintptr_t lo[2] = {UINTPTR_MAX, UINTPTR_MAX}, hi[2] = {0, 0};
+    for (int i = 0; i < na; ++i) {
+        lo[0] = (uintptr_t)a[i] < lo[0] ? (uintptr_t)a[i] : lo[0];
+        hi[0] = (uintptr_t)a[i] + a_bytes > hi[0] ? (uintptr_t)a[i] + a_bytes : hi[0];
+    }
+    for (int i = 0; i < nb; ++i) {
+        lo[1] = (uintptr_t)b[i] < lo[1] ? (uintptr_t)b[i] : lo[1];
+        hi[1] = (uintptr_t)b[i] + b_bytes > hi[1] ? (uintptr_t)b[i] + b_bytes : hi[1];
+    }
+    if (lo[0] >= hi[1] || lo[1] >= hi[0]) return false;
+    for (int i = 0; i < na; ++i)
+        for (int j = 0; j < nb; ++j)
+            if (overlaps(a[i], a_bytes, b[j], b_bytes)) return true;
+    return false;
+}
+
+struct MoveCall {
+    const void* const* k;  // wide tensors
+    const void* const* v;
+    const void* const* cache;
+    const civic_row_strides_t* strides;
+    int32_t n_layers, n_seq, n_rows, wide_rows;
+    const int32_t* idx;
+    const int32_t* start;
+    const int32_t* counts;
+    const civic_quant_desc_t* desc;
+    const int32_t* block_table;
+    int32_t max_pages;
+    bool writes_cache;
+};
+
+template <typename T, int HD, int BITS>
+cudaError_t launch_move(bool write, const civic::QuantMoveParams& p, dim3 grid, cudaStream_t stream)
+{
+    return write ? civic::launch(programmatic(), civic::quant_write_kernel<T, HD, BITS>, grid, civic::kQuantThreads, 0, stream, p)
+                 : civic::launch(programmatic(), civic::quant_read_kernel<T, HD, BITS>, grid, civic::kQuantThreads, 0, stream, p);
+}
+template <typename T, int HD>
+cudaError_t launch_move_bits(int bits, bool write, const civic::QuantMoveParams& p, dim3 grid, cudaStream_t stream)
+{
+    return bits == 4 ? launch_move<T, HD, 4>(write, p, grid, stream) : launch_move<T, HD, 8>(write, p, grid, stream);
+}
+template <typename T>
+cudaError_t launch_move_dim(const civic_quant_desc_t& d, bool write, const civic::QuantMoveParams& p, dim3 grid, cudaStream_t stream)
+{
+    switch (d.head_dim) {
+        case 64: return launch_move_bits<T, 64>(d.bits, write, p, grid, stream);
+        case 128: return launch_move_bits<T, 128>(d.bits, write, p, grid, stream);
+        default: return launch_move_bits<T, 256>(d.bits, write, p, grid, stream);
+    }
+}
+
+civic_status_t move_impl(const MoveCall& c, void* stream_)
+{
+    civic_status_t st = check_desc(c.desc);
+    if (st != CIVIC_OK) return st;
+    if (c.n_layers < 1 || c.n_seq < 0 || c.n_rows < 0 || c.max_pages < 0) return CIVIC_ERR_INVALID_ARG;
+    st = check_strides(c.strides);
+    if (st != CIVIC_OK) return st;
+    const civic_quant_desc_t& d = *c.desc;
+    if (c.n_seq == 0 || c.n_rows == 0) return CIVIC_OK;
+    if (!c.k || !c.v || !c.cache || !c.block_table) return CIVIC_ERR_INVALID_ARG;
+    if (!aligned(c.block_table, 4) || !aligned(c.idx, 4) || !aligned(c.start, 4) || !aligned(c.counts, 4))
+        return CIVIC_ERR_ALIGNMENT;
+    for (int l = 0; l < c.n_layers; ++l) {
+        if (!c.k[l] || !c.v[l] || !c.cache[l]) return CIVIC_ERR_INVALID_ARG;
+        if (!aligned(c.k[l], 16) || !aligned(c.v[l], 16) || !aligned(c.cache[l], 16)) return CIVIC_ERR_ALIGNMENT;
+        if (!c.writes_cache && c.k[l] == c.v[l]) return CIVIC_ERR_INVALID_ARG;
+    }
+    if (!c.writes_cache && !writable_strides(*c.strides, c.n_seq, c.n_rows, d.n_heads, d.head_dim)) return CIVIC_ERR_INVALID_ARG;
+    if (c.wide_rows > 0) {
+        const size_t wide = extent_bytes(*c.strides, c.n_seq, c.wide_rows, d.n_heads, d.head_dim);
+        const size_t cache = (size_t)d.n_pages * page_bytes(d);
+        if (lists_overlap(c.k, c.n_layers, wide, c.cache, c.n_layers, cache) ||
+            lists_overlap(c.v, c.n_layers, wide, c.cache, c.n_layers, cache))
+            return CIVIC_ERR_INVALID_ARG;
+        const void* small[4] = {c.block_table, c.idx, c.start, c.counts};
+        const size_t bytes[4] = {(size_t)c.n_seq * c.max_pages * 4, (size_t)c.n_seq * c.n_rows * 4, (size_t)c.n_seq * 4,
+                                 (size_t)c.n_seq * 4};
+        for (int i = 0; i < 4; ++i) {
+            if (!small[i]) continue;
+            const void* const one[1] = {small[i]};
+            if (c.writes_cache ? lists_overlap(c.cache, c.n_layers, cache, one, 1, bytes[i])
+                               : lists_overlap(c.k, c.n_layers, wide, one, 1, bytes[i]) ||
+                                     lists_overlap(c.v, c.n_layers, wide, one, 1, bytes[i]))
+                return CIVIC_ERR_INVALID_ARG;
+        }
+        if (c.writes_cache)
+            for (int a = 0; a + 1 < c.n_layers; ++a) {
+                // neighbours in ascending order cannot meet; any other order is looked at pair by pair
+                if ((uintptr_t)c.cache[a] + cache <= (uintptr_t)c.cache[a + 1] && a + 2 == c.n_layers) break;
+                if ((uintptr_t)c.cache[a] + cache <= (uintptr_t)c.cache[a + 1]) continue;
+                for (int x = 0; x < c.n_layers; ++x)
+                    for (int y = x + 1; y < c.n_layers; ++y)
+                        if (overlaps(c.cache[x], cache, c.cache[y], cache)) return CIVIC_ERR_INVALID_ARG;
+                break;
+            }
+    }
+    civic::QuantMoveParams p;
+    memset(&p, 0, sizeof p);
+    // rows that start inside a tile can reach one tile more
+    const int64_t span = (int64_t)c.n_rows + (c.start ? civic::kQuantTile - 1 : 0);
+    const int64_t tiles = (span + civic::kQuantTile - 1) / civic::kQuantTile;
+    const int64_t units = tiles * c.n_seq * d.n_heads;
+    if (tiles > INT32_MAX || c.n_seq > INT32_MAX / (tiles * d.n_heads) || units > INT32_MAX) return CIVIC_ERR_UNSUPPORTED;
+    p.idx = c.idx;
+    p.start = c.start;
+    p.counts = c.counts;
+    p.block_table = c.block_table;
+    p.seq_stride = c.strides->seq * 2;
+    p.token_stride = c.strides->token * 2;
+    p.head_stride = c.strides->head * 2;
+    p.n_units = (uint32_t)units;
+    p.n_heads = d.n_heads;
+    p.tiles = (int32_t)tiles;
+    p.n_rows = c.n_rows;
+    p.wide_rows = c.wide_rows;
+    p.page_tiles = d.page_size / civic::kQuantTile;
+    p.max_pages = c.max_pages;
+    p.n_pages = d.n_pages;
+    p.check = g_index_check;
+    const unsigned warps = civic::kQuantThreads / 32;
+    for (int l0 = 0; l0 < c.n_layers; l0 += civic::kMaxQuantLayers) {
+        const int nl = c.n_layers - l0 < civic::kMaxQuantLayers ? c.n_layers - l0 : civic::kMaxQuantLayers;
+        for (int l = 0; l < nl; ++l) {
+            p.wide[2 * l] = (char*)const_cast<void*>(c.k[l0 + l]);
+            p.wide[2 * l + 1] = (char*)const_cast<void*>(c.v[l0 + l]);
+            p.cache[l] = (char*)const_cast<void*>(c.cache[l0 + l]);
+        }
+        const dim3 grid((p.n_units + warps - 1) / warps, 2u * nl);
+        CIVIC_CUDA_TRY(d.dtype == CIVIC_BF16
+                           ? launch_move_dim<__nv_bfloat16>(d, c.writes_cache, p, grid, (cudaStream_t)stream_)
+                           : launch_move_dim<__half>(d, c.writes_cache, p, grid, (cudaStream_t)stream_));
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+    }
+    return CIVIC_OK;
+}
+
+// Column tiles of 8 query rows that a warp of the attention kernel takes at once: enough for all
+// rows of a K/V head, as far as registers hold the accumulators (HD / 16 * 4 for each).
+int attention_tiles(int head_dim, int64_t rows)
+{
+    const int most = head_dim == 64 ? 4 : (head_dim == 128 ? 2 : 1);
+    int nt = 1;
+    while (nt < most && rows > 8 * nt) nt *= 2;
+    return nt;
+}
+
+template <typename T, int HD, int BITS, int NT>
+civic_status_t launch_attention(civic::QuantAttnParams& p, unsigned items, cudaStream_t stream)
+{
+    const auto kernel = civic::quant_attention_kernel<T, HD, BITS, NT>;
+    constexpr size_t smem = civic::qa_smem_bytes<HD, BITS, NT>();
+    static_assert(smem <= kMaxDynamicSmem, "the ring and the join area fit into shared memory");
+    static std::atomic<int> allowed[64], resident[64];
+    const civic_status_t as = allow_dynamic_smem(kernel, smem, allowed);
+    if (as != CIVIC_OK) return as;
+    const int dev = device_slot();
+    int per_sm = dev >= 0 ? resident[dev].load(std::memory_order_relaxed) : 0;
+    if (per_sm == 0) {
+        CIVIC_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, civic::kQaThreads, smem));
+        if (per_sm < 1) return CIVIC_ERR_UNSUPPORTED;
+        if (dev >= 0) resident[dev].store(per_sm, std::memory_order_relaxed);
+    }
+    const int blocks = sm_count() * per_sm;
+    p.blocks = blocks < civic::kQaMaxBlocks ? blocks : civic::kQaMaxBlocks;
+    const bool pdl = programmatic();
+    CIVIC_CUDA_TRY(civic::launch(pdl, kernel, (unsigned)p.blocks, (unsigned)civic::kQaThreads, smem, stream, p));
+    CIVIC_CUDA_TRY(civic::launch(pdl, civic::quant_attention_join_kernel<T, HD, NT>, dim3(items, (unsigned)p.n_seq),
+                                 (unsigned)(HD / 4 * 8), 0, stream, p));
+    g_launches.fetch_add(2, std::memory_order_relaxed);
+    return CIVIC_OK;
+}
+template <typename T, int HD, int NT>
+civic_status_t launch_attention_bits(int bits, civic::QuantAttnParams& p, unsigned items, cudaStream_t stream)
+{
+    return bits == 4 ? launch_attention<T, HD, 4, NT>(p, items, stream) : launch_attention<T, HD, 8, NT>(p, items, stream);
+}
+template <typename T>
+civic_status_t launch_attention_dim(const civic_quant_desc_t& d, int nt, civic::QuantAttnParams& p, unsigned items,
+                                    cudaStream_t stream)
+{
+    if (d.head_dim == 64)
+        return nt == 1 ? launch_attention_bits<T, 64, 1>(d.bits, p, items, stream)
+                       : (nt == 2 ? launch_attention_bits<T, 64, 2>(d.bits, p, items, stream)
+                                  : launch_attention_bits<T, 64, 4>(d.bits, p, items, stream));
+    if (d.head_dim == 128)
+        return nt == 1 ? launch_attention_bits<T, 128, 1>(d.bits, p, items, stream)
+                       : launch_attention_bits<T, 128, 2>(d.bits, p, items, stream);
+    return launch_attention_bits<T, 256, 1>(d.bits, p, items, stream);
+}
+
+civic_status_t check_attention(const civic_quant_desc_t* desc, int32_t n_seq, int32_t q_len, int32_t q_heads)
+{
+    const civic_status_t st = check_desc(desc);
+    if (st != CIVIC_OK) return st;
+    if (n_seq < 0 || q_len < 0 || q_heads < 1 || q_heads % desc->n_heads) return CIVIC_ERR_INVALID_ARG;
+    // grid limits; a sequence's query rows are counted in 32 bits
+    if (n_seq > 65535 || (int64_t)q_len * q_heads > (1 << 24)) return CIVIC_ERR_UNSUPPORTED;
+    return CIVIC_OK;
+}
+
+size_t attention_workspace(const civic_quant_desc_t& d, int32_t q_len, int32_t q_heads)
+{
+    const int nt = attention_tiles(d.head_dim, (int64_t)q_len * (q_heads / d.n_heads));
+    return round_up((size_t)2 * civic::kQaMaxBlocks * 8 * nt * (d.head_dim + 2) * 4, 256);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t civic_quant_page_bytes(const civic_quant_desc_t* desc) { return check_desc(desc) == CIVIC_OK ? page_bytes(*desc) : 0; }
+
+civic_status_t civic_compact_kv_quant(const void* const* k_src, const void* const* v_src, const civic_row_strides_t* src_strides,
+                                      int32_t n_layers, int32_t n_seq, int32_t seq_len, int32_t s_out, const int32_t* seq_idx,
+                                      void* const* cache, const civic_quant_desc_t* desc, const int32_t* block_table,
+                                      int32_t max_pages_per_seq, void* stream)
+{
+    const civic_status_t st = check_desc(desc);
+    if (st != CIVIC_OK) return st;
+    if (seq_len < 0 || (n_seq > 0 && s_out > 0 && !seq_idx)) return CIVIC_ERR_INVALID_ARG;
+    if ((int64_t)max_pages_per_seq * desc->page_size < s_out) return CIVIC_ERR_INVALID_ARG;
+    const MoveCall c{k_src, v_src, (const void* const*)cache, src_strides, n_layers, n_seq, s_out, seq_len, seq_idx, nullptr,
+                     nullptr, desc, block_table, max_pages_per_seq, true};
+    return move_impl(c, stream);
+}
+
+civic_status_t civic_append_kv_quant(const void* const* k_new, const void* const* v_new, const civic_row_strides_t* src_strides,
+                                     int32_t n_layers, int32_t n_seq, int32_t n_new, const int32_t* start, const int32_t* counts,
+                                     void* const* cache, const civic_quant_desc_t* desc, const int32_t* block_table,
+                                     int32_t max_pages_per_seq, void* stream)
+{
+    if (n_seq > 0 && n_new > 0 && !start) return CIVIC_ERR_INVALID_ARG;
+    const MoveCall c{k_new, v_new, (const void* const*)cache, src_strides, n_layers, n_seq, n_new, n_new, nullptr, start,
+                     counts, desc, block_table, max_pages_per_seq, true};
+    return move_impl(c, stream);
+}
+
+civic_status_t civic_read_kv_quant(const void* const* cache, const civic_quant_desc_t* desc, const int32_t* block_table,
+                                   int32_t max_pages_per_seq, int32_t n_layers, int32_t n_seq, int32_t max_rows,
+                                   const int32_t* start, const int32_t* counts, void* const* k_dst, void* const* v_dst,
+                                   const civic_row_strides_t* dst_strides, void* stream)
+{
+    if (n_seq > 0 && max_rows > 0 && !counts) return CIVIC_ERR_INVALID_ARG;
+    const MoveCall c{(const void* const*)k_dst, (const void* const*)v_dst, cache, dst_strides, n_layers, n_seq, max_rows, max_rows,
+                     nullptr, start, counts, desc, block_table, max_pages_per_seq, false};
+    return move_impl(c, stream);
+}
+
+size_t civic_quant_attention_workspace_bytes(const civic_quant_desc_t* desc, int32_t n_seq, int32_t q_len, int32_t q_heads)
+{
+    return check_attention(desc, n_seq, q_len, q_heads) == CIVIC_OK ? attention_workspace(*desc, q_len, q_heads) : 0;
+}
+
+civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q_strides, const void* cache,
+                                     const civic_quant_desc_t* desc, const int32_t* block_table, int32_t max_pages_per_seq,
+                                     const int32_t* lens, const int32_t* q_lens, int32_t n_seq, int32_t q_len, int32_t q_heads,
+                                     float scale, int32_t causal, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                     void* stream)
+{
+    civic_status_t st = check_attention(desc, n_seq, q_len, q_heads);
+    if (st != CIVIC_OK) return st;
+    st = check_strides(q_strides);
+    if (st != CIVIC_OK) return st;
+    if (max_pages_per_seq < 0 || !std::isfinite(scale)) return CIVIC_ERR_INVALID_ARG;
+    const civic_quant_desc_t& d = *desc;
+    if ((int64_t)max_pages_per_seq * d.page_size > INT32_MAX - 64) return CIVIC_ERR_UNSUPPORTED;
+    if (n_seq == 0 || q_len == 0) return CIVIC_OK;
+    if (!q || !cache || !lens || !out || (!block_table && max_pages_per_seq > 0)) return CIVIC_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(cache, 16) || !aligned(out, 16) || !aligned(block_table, 4) || !aligned(lens, 4) ||
+        !aligned(q_lens, 4) || !aligned(lse, 4))
+        return CIVIC_ERR_ALIGNMENT;
+    const size_t need = attention_workspace(d, q_len, q_heads);
+    if (!workspace || workspace_bytes < need) return CIVIC_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return CIVIC_ERR_ALIGNMENT;
+    {
+        const size_t rows = (size_t)n_seq * q_len * q_heads;
+        const void* made[3] = {out, lse, workspace};
+        const size_t made_bytes[3] = {rows * d.head_dim * 2, rows * 4, need};
+        const void* given[5] = {q, cache, block_table, lens, q_lens};
+        const size_t given_bytes[5] = {extent_bytes(*q_strides, n_seq, q_len, q_heads, d.head_dim), (size_t)d.n_pages * page_bytes(d),
+                                       (size_t)n_seq * max_pages_per_seq * 4, (size_t)n_seq * 4, (size_t)n_seq * 4};
+        for (int a = 0; a < 3; ++a) {
+            for (int b = 0; b < 5; ++b)
+                if (overlaps(made[a], made_bytes[a], given[b], given_bytes[b])) return CIVIC_ERR_INVALID_ARG;
+            for (int b = a + 1; b < 3; ++b)
+                if (overlaps(made[a], made_bytes[a], made[b], made_bytes[b])) return CIVIC_ERR_INVALID_ARG;
+        }
+    }
+    civic::QuantAttnParams p;
+    memset(&p, 0, sizeof p);
+    p.q = (const char*)q;
+    p.cache = (const char*)cache;
+    p.block_table = block_table;
+    p.lens = lens;
+    p.q_lens = q_lens;
+    p.out = (char*)out;
+    p.lse = lse;
+    p.partial = (float*)workspace;
+    p.q_seq = q_strides->seq * 2;
+    p.q_token = q_strides->token * 2;
+    p.q_head = q_strides->head * 2;
+    p.n_seq = n_seq;
+    p.q_len = q_len;
+    p.q_heads = q_heads;
+    p.n_heads = d.n_heads;
+    p.group = q_heads / d.n_heads;
+    p.causal = causal != 0;
+    p.page_tiles = d.page_size / civic::kQuantTile;
+    p.max_pages = max_pages_per_seq;
+    p.n_pages = d.n_pages;
+    p.capacity = max_pages_per_seq * d.page_size;
+    p.scale_log2e = scale * 1.4426950408889634f;
+    p.check = g_index_check;
+    const int64_t rows = (int64_t)q_len * p.group;
+    const int nt = attention_tiles(d.head_dim, rows);
+    const unsigned items = (unsigned)((rows + 8 * nt - 1) / (8 * nt) * d.n_heads);
+    return d.dtype == CIVIC_BF16 ? launch_attention_dim<__nv_bfloat16>(d, nt, p, items, (cudaStream_t)stream)
+                                 : launch_attention_dim<__half>(d, nt, p, items, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,692 @@
+// Attention over the quantised paged K/V cache (quant_cache.cuh), for one query token or several:
+//
+//     S_j = scale * q . k_j,   out = sum_j exp(S_j - lse) v_j,   lse = log sum_j exp S_j
+//
+// over the tokens that a query row sees.  With k = s c + m per group of 32 channels (c the code),
+//     q . k = sum over groups of  s (q . c) + m (sum of q over the group),
+// so the matrix instruction multiplies q with the bare codes, and scale and minimum act on its 32-bit
+// results, once per token, group and query row.  For V they act on the weights: P' = p s goes into
+// the second product, and the minima add one sum per group, sum_j p_j m_j.  A code becomes a
+// matrix operand by one AND for two codes: as the low bits of an fp16 it is the subnormal
+// c * 2^-24 (an odd nibble 16 c * 2^-24), and the power of two comes off the 32-bit result.
+//
+// Products are 16 x 8 x 16 (mma.sync): S^T = K Q^T has 16 tokens for rows, 8 query rows for columns;
+// O^T = V^T P'^T has 16 channels for rows, 16 tokens of depth.  The codes fill the 16 x 16 operand,
+// so that no part of it is idle when a K/V head serves fewer than 8 query rows.  One movmatrix turns
+// P' from the first product's result layout into the second's operand.
+//
+// fp16 operands, 32-bit accumulators and statistics.  q is scaled by a power of two per row, so that
+// its largest element is in [2^14, 2^15): elements down to 2^-28 of it are still represented.  P' is
+// rounded to fp16 (11 bits): its reference exponent m bounds S + log2(s), not S alone, so that the
+// largest product p s, not the largest p, is near 1.  The reference is lazy: it moves only when some
+// S + log2(s) exceeds it by more than 8 (a warp vote), and then O, l and the minima's sums follow.
+//
+// Work split: all (sequence, K/V head, block of query rows) items' tiles of 16 tokens in one line, cut
+// into equal shares, one per block, computed on the device from the lengths, so ragged batches
+// balance themselves and the lengths stay on the device.  A block's warps take the tiles of its
+// share in turn, each with its own ring of tiles in shared memory that cp.async fills ahead.
+// Shares that cut an item leave partial results (m, l, O) in the workspace, and a second small kernel
+// joins them in a fixed order.
+#pragma once
+#include "quant_cache.cuh"
+
+namespace civic {
+
+constexpr int kQaWarps = 4;
+constexpr int kQaThreads = 32 * kQaWarps;
+constexpr int kQaMaxBlocks = 148 * 4;  // also fixes the workspace size
+constexpr int kQaMinTiles = 2 * kQaWarps;
+constexpr float kQaNoMax = -1e30f;     // reference of a row that has seen nothing
+constexpr float kQaSlack = 8.f;        // P' stays below 2^9
+
+struct QuantAttnParams {
+    const char* q;
+    const char* cache;
+    const int32_t* block_table;
+    const int32_t* lens;
+    const int32_t* q_lens;       // or NULL = q_len everywhere
+    char* out;                   // [n_seq, q_len, q_heads, HD]
+    float* lse;                  // [n_seq, q_len, q_heads] or NULL
+    float* partial;              // [2 * blocks][rows][HD + 2]
+    int64_t q_seq, q_token, q_head;  // strides in bytes
+    int32_t n_seq, q_len, q_heads, n_heads, group;
+    int32_t causal;
+    int32_t page_tiles, max_pages, n_pages;
+    int32_t capacity;            // tokens the block table can address
+    int32_t blocks;              // of the main kernel
+    float scale_log2e;
+    int32_t* check;
+};
+
+struct QaSeq {
+    int len, q_len, tiles, row_blocks;
+    long long units;  // tiles * heads * row blocks
+};
+
+template <int ROWS>
+__device__ __forceinline__ QaSeq qa_sequence(const QuantAttnParams& p, int s)
+{
+    QaSeq q;
+    q.len = min(max(__ldg(p.lens + s), 0), p.capacity);
+    q.q_len = p.q_lens ? min(max(__ldg(p.q_lens + s), 0), p.q_len) : p.q_len;
+    q.tiles = (q.len + kQuantTile - 1) / kQuantTile;
+    q.row_blocks = (q.q_len * p.group + ROWS - 1) / ROWS;
+    q.units = (long long)q.tiles * q.row_blocks * p.n_heads;
+    return q;
+}
+
+__device__ __forceinline__ long long warp_scan_add(long long v, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long o = __shfl_up_sync(0xFFFFFFFFu, v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+// Units of the whole call, and units of the sequences before `upto`; by a whole warp.
+template <int ROWS>
+__device__ __forceinline__ long long qa_total(const QuantAttnParams& p, int upto, long long& before)
+{
+    const int lane = threadIdx.x & 31;
+    long long total = 0;
+    before = 0;
+    for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
+        const int s = s0 + lane;
+        long long u = s < p.n_seq ? qa_sequence<ROWS>(p, s).units : 0, b = s < upto ? u : 0;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            u += __shfl_xor_sync(0xFFFFFFFFu, u, d);
+            b += __shfl_xor_sync(0xFFFFFFFFu, b, d);
+        }
+        total += u;
+        before += b;
+    }
+    return total;
+}
+
+__host__ __device__ inline long long qa_share(long long total, int blocks)
+{
+    const long long even = (total + blocks - 1) / blocks;
+    return even < kQaMinTiles ? kQaMinTiles : even;
+}
+
+// A place in the line of units.
+struct QaCursor {
+    int seq, item, tile;  // item = head * row_blocks + row block
+    QaSeq q;
+};
+
+template <int ROWS>
+__device__ __forceinline__ QaCursor qa_locate(const QuantAttnParams& p, long long unit)
+{
+    const int lane = threadIdx.x & 31;
+    long long before = 0;
+    QaCursor c;
+    c.seq = p.n_seq;
+    for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
+        const int s = s0 + lane;
+        const long long u = s < p.n_seq ? qa_sequence<ROWS>(p, s).units : 0;
+        const long long upto = before + warp_scan_add(u, lane);
+        const unsigned past = __ballot_sync(0xFFFFFFFFu, upto > unit);
+        if (past) {
+            const int l = __ffs(past) - 1;
+            const long long rest = unit - __shfl_sync(0xFFFFFFFFu, upto - u, l);
+            c.seq = s0 + l;
+            c.q = qa_sequence<ROWS>(p, c.seq);
+            c.item = (int)(rest / c.q.tiles);
+            c.tile = (int)(rest - (long long)c.item * c.q.tiles);
+            return c;
+        }
+        before = __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    return c;
+}
+
+template <int ROWS>
+__device__ __forceinline__ void qa_advance(const QuantAttnParams& p, QaCursor& c, int by)
+{
+    c.tile += by;
+    while (c.seq < p.n_seq && c.tile >= c.q.tiles) {
+        c.tile -= c.q.tiles;
+        if (++c.item < c.q.row_blocks * p.n_heads) continue;
+        c.item = 0;
+        do {
+            if (++c.seq >= p.n_seq) return;
+            c.q = qa_sequence<ROWS>(p, c.seq);
+        } while (c.q.units == 0);
+    }
+}
+
+// ---- matrix instructions ---------------------------------------------------------------------------
+
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                            uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
+{
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) { return Half16<__half>::pack(lo, hi); }
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void cp_async16(void* dst, const void* src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// ---- one warp's running state for one item -----------------------------------------------------------
+
+template <typename T, int HD, int BITS, int NT>
+struct QaWarp {
+    using Tile = QuantTile<HD, BITS>;
+    using H = Half16<T>;
+    static constexpr int NG = Tile::kGroups, MT = HD / 16;
+
+    uint32_t q[NT][NG][2][2];  // operand of the first product: [group][depth step][register]
+    float q_sum[NT][2][NG];    // sum over the group of the scaled q, times 2^-24; columns 2 t, 2 t + 1
+    float factor[NT][2];       // takes a raw score to base-2 logits
+    int limit[NT][2];          // tokens the column's query row sees
+    float ref[NT][2], l[NT][2], v_min[NT][2][NG];
+    float o[NT][MT][4];
+
+    __device__ __forceinline__ void begin(const QuantAttnParams& p, const QaCursor& c)
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const int head = c.item / c.q.row_blocks, row0 = (c.item - head * c.q.row_blocks) * (8 * NT);
+        const int rows = c.q.q_len * p.group;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = row0 + nt * 8 + g, token = row / p.group, sub = row - token * p.group;
+            uint4 x[NG];
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                x[j] = make_uint4(0, 0, 0, 0);
+                if (row < rows)
+                    x[j] = __ldg(reinterpret_cast<const uint4*>(p.q + c.seq * p.q_seq + token * p.q_token +
+                                                                (head * p.group + sub) * p.q_head + (j * 32 + t * 8) * 2));
+            }
+            // the row's power of two
+            float top = 0.f;
+            float f[NG][8];
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                const uint32_t w[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    f[j][i] = (i & 1) ? H::hi(w[i >> 1]) : H::lo(w[i >> 1]);
+                    top = fmaxf(top, fabsf(f[j][i]));
+                }
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 126);
+            const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23), down = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+            float sums[NG];
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    f[j][i] *= up;
+                    sum += f[j][i];
+                }
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                sums[j] = sum * 0x1p-24f;
+                if constexpr (BITS == 4) {
+                    // nibbles i and i + 4 of a word meet in one operand register; odd ones arrive times 16
+                    q[nt][j][0][0] = pack_half2(f[j][0], f[j][4]);
+                    q[nt][j][0][1] = pack_half2(f[j][1] * 0.0625f, f[j][5] * 0.0625f);
+                    q[nt][j][1][0] = pack_half2(f[j][2], f[j][6]);
+                    q[nt][j][1][1] = pack_half2(f[j][3] * 0.0625f, f[j][7] * 0.0625f);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        q[nt][j][h][0] = pack_half2(f[j][4 * h], f[j][4 * h + 2]);
+                        q[nt][j][h][1] = pack_half2(f[j][4 * h + 1], f[j][4 * h + 3]);
+                    }
+                }
+            }
+            // what belongs to a column of the score tile: from the lanes that hold its query row
+            const float fac = down * 0x1p24f * p.scale_log2e;
+            const int seen = row < rows ? (p.causal ? min(max(c.q.len - c.q.q_len + token + 1, 0), c.q.len) : c.q.len) : 0;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int from = (2 * t + b) * 4;
+                factor[nt][b] = __shfl_sync(0xFFFFFFFFu, fac, from);
+                limit[nt][b] = __shfl_sync(0xFFFFFFFFu, seen, from);
+                ref[nt][b] = kQaNoMax;
+                l[nt][b] = 0.f;
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    q_sum[nt][b][j] = __shfl_sync(0xFFFFFFFFu, sums[j], from);
+                    v_min[nt][b][j] = 0.f;
+                }
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[nt][mt][i] = 0.f;
+        }
+    }
+
+    // WORDS 32-bit words from 16-, 8-byte aligned shared memory
+    template <int WORDS>
+    __device__ __forceinline__ static void load(uint32_t (&w)[WORDS], const uint32_t* at)
+    {
+        if constexpr (WORDS == 2) {
+            const uint2 v = *reinterpret_cast<const uint2*>(at);
+            w[0] = v.x;
+            w[1] = v.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(at + i);
+                w[i] = v.x;
+                w[i + 1] = v.y;
+                w[i + 2] = v.z;
+                w[i + 3] = v.w;
+            }
+        }
+    }
+
+    // Tile of the 16 tokens from `pos` on; MASK: some column does not see all of them.
+    template <bool MASK>
+    __device__ __forceinline__ void step(const uint8_t* tile, int pos)
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const uint32_t* kc = reinterpret_cast<const uint32_t*>(tile);
+        const uint32_t* vc = reinterpret_cast<const uint32_t*>(tile + Tile::kVCodes);
+        const uint32_t* kp = reinterpret_cast<const uint32_t*>(tile + Tile::kKParams);
+        const uint32_t* vp = reinterpret_cast<const uint32_t*>(tile + Tile::kVParams);
+        // ---- scores: c[nt] = rows g and g + 8 (tokens), columns 2 t and 2 t + 1 (query rows)
+        float c[NT][4] = {};
+        {
+            uint32_t par[2][NG];
+            load(par[0], kp + g * NG);
+            load(par[1], kp + (g + 8) * NG);
+#pragma unroll
+            for (int pl = 0; pl < Tile::kPlanes; ++pl) {
+                uint32_t w[2][Tile::kPlane];
+                load(w[0], kc + Tile::k_word(g, t, pl * Tile::kPlane));
+                load(w[1], kc + Tile::k_word(g + 8, t, pl * Tile::kPlane));
+#pragma unroll
+                for (int jj = 0; jj < Tile::kPlane * 4 / BITS; ++jj) {
+                    const int j = pl * (Tile::kPlane * 4 / BITS) + jj;
+                    uint32_t a[2][4];
+                    if constexpr (BITS == 4) {
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const uint32_t x = w[r][jj], y = x >> 8;
+                            a[0][r] = x & 0x000F000Fu;
+                            a[0][2 + r] = x & 0x00F000F0u;
+                            a[1][r] = y & 0x000F000Fu;
+                            a[1][2 + r] = y & 0x00F000F0u;
+                        }
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const uint32_t x = w[r][2 * jj + h];
+                                a[h][r] = x & 0x00FF00FFu;
+                                a[h][2 + r] = (x >> 8) & 0x00FF00FFu;
+                            }
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            mma_16x8x16(d, a[h][0], a[h][1], a[h][2], a[h][3], q[nt][j][h][0], q[nt][j][h][1]);
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+#pragma unroll
+                            for (int b = 0; b < 2; ++b)
+                                c[nt][2 * r + b] += H::lo(par[r][j]) * d[2 * r + b] + H::hi(par[r][j]) * q_sum[nt][b][j];
+                    }
+                }
+            }
+        }
+        // ---- softmax against the running reference
+        uint32_t par[2][NG];
+        load(par[0], vp + g * NG);
+        load(par[1], vp + (g + 8) * NG);
+        float lift[2];  // about log2 of the token's largest V scale
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float s = H::lo(par[r][0]);
+#pragma unroll
+            for (int j = 1; j < NG; ++j) s = fmaxf(s, H::lo(par[r][j]));
+            lift[r] = (float)min(max((int)(__float_as_uint(s) >> 23) - 126, -90), 90);
+        }
+        bool move = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    float& s = c[nt][2 * r + b];
+                    s *= factor[nt][b];
+                    if (MASK && pos + g + 8 * r >= limit[nt][b]) s = -INFINITY;
+                    move |= s + lift[r] > ref[nt][b] + kQaSlack;
+                }
+            }
+        if (__any_sync(0xFFFFFFFFu, move)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float top = fmaxf(c[nt][b] + lift[0], c[nt][2 + b] + lift[1]);
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                    top = fmaxf(top, ref[nt][b]);
+                    const float f = exp2_fast(ref[nt][b] - top);
+                    ref[nt][b] = top;
+                    l[nt][b] *= f;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) v_min[nt][b][j] *= f;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        o[nt][mt][b] *= f;
+                        o[nt][mt][2 + b] *= f;
+                    }
+                }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    float& x = c[nt][2 * r + b];
+                    x = exp2_fast(x - ref[nt][b]);
+                    l[nt][b] += x;
+                }
+        // ---- O^T += V^T P'^T, group by group
+#pragma unroll
+        for (int pl = 0; pl < Tile::kPlanes; ++pl) {
+            uint32_t w[2][Tile::kPlane];
+            load(w[0], vc + Tile::v_word(0, lane, pl * Tile::kPlane));
+            load(w[1], vc + Tile::v_word(1, lane, pl * Tile::kPlane));
+#pragma unroll
+            for (int jj = 0; jj < Tile::kPlane * 4 / BITS; ++jj) {
+                const int j = pl * (Tile::kPlane * 4 / BITS) + jj;
+                uint32_t a[2][4];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if constexpr (BITS == 4) {
+                        const uint32_t x = w[k][jj], y = x >> 8;
+                        a[0][2 * k] = x & 0x000F000Fu;
+                        a[0][2 * k + 1] = x & 0x00F000F0u;
+                        a[1][2 * k] = y & 0x000F000Fu;
+                        a[1][2 * k + 1] = y & 0x00F000F0u;
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t x = w[k][2 * jj + h];
+                            a[h][2 * k] = x & 0x00FF00FFu;
+                            a[h][2 * k + 1] = (x >> 8) & 0x00FF00FFu;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float x[4];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const float w_p = c[nt][2 * r + b];
+                            float scaled = w_p * H::lo(par[r][j]), low = w_p * H::hi(par[r][j]);
+                            if (MASK && pos + g + 8 * r >= limit[nt][b]) scaled = low = 0.f;  // whatever the tile holds there
+                            x[2 * r + b] = scaled;
+                            v_min[nt][b][j] += low;
+                        }
+                    const uint32_t b0 = transpose_8x8(pack_half2(x[0], x[1])), b1 = transpose_8x8(pack_half2(x[2], x[3]));
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) mma_16x8x16(o[nt][2 * j + h], a[h][0], a[h][1], a[h][2], a[h][3], b0, b1);
+                }
+            }
+        }
+    }
+
+    // Sums over the lanes that share a column; then every lane of a column's quad has them.
+    __device__ __forceinline__ void finish()
+    {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    l[nt][b] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][b], d);
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) v_min[nt][b][j] += __shfl_xor_sync(0xFFFFFFFFu, v_min[nt][b][j], d);
+                }
+    }
+    // Channels 32 j + 4 g .. + 3 of column b.
+    __device__ __forceinline__ float4 output(int nt, int b, int j) const
+    {
+        constexpr float kOdd = BITS == 4 ? 0x1p20f : 0x1p24f;
+        const float m = v_min[nt][b][j];
+        return make_float4(fmaf(o[nt][2 * j][b], 0x1p24f, m), fmaf(o[nt][2 * j][2 + b], kOdd, m),
+                           fmaf(o[nt][2 * j + 1][b], 0x1p24f, m), fmaf(o[nt][2 * j + 1][2 + b], kOdd, m));
+    }
+};
+
+template <int HD, int BITS>
+__host__ __device__ constexpr int qa_stages()
+{
+    const int n = 12288 / quant_tile_bytes(HD, BITS);
+    return n < 2 ? 2 : (n > 6 ? 6 : n);
+}
+// ring | O of every warp, one n-tile at a time | reference and sum of every warp and row
+template <int HD, int BITS, int NT>
+__host__ __device__ constexpr size_t qa_smem_bytes()
+{
+    return (size_t)kQaWarps * (qa_stages<HD, BITS>() * quant_tile_bytes(HD, BITS) + 8 * HD * 4 + NT * 8 * 8);
+}
+
+// out and lse of one row from the sums over its tokens
+template <typename T>
+__device__ __forceinline__ void qa_store(const QuantAttnParams& p, int seq, int head, int row, int channel, int hd, float4 o, float m,
+                                         float l)
+{
+    const int token = row / p.group, h = head * p.group + row - token * p.group;
+    const size_t at = ((size_t)seq * p.q_len + token) * p.q_heads + h;
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
+    const uint2 v = make_uint2(Half16<T>::pack(o.x * inv, o.y * inv), Half16<T>::pack(o.z * inv, o.w * inv));
+    *reinterpret_cast<uint2*>(p.out + (at * hd + channel) * 2) = v;
+    if (channel == 0 && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+template <typename T, int HD, int BITS, int NT>
+__global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __grid_constant__ QuantAttnParams p)
+{
+    using Tile = QuantTile<HD, BITS>;
+    constexpr int kStages = qa_stages<HD, BITS>(), kRows = 8 * NT;
+    extern __shared__ __align__(16) uint8_t qa_smem[];
+    uint8_t* ring_all = qa_smem;
+    float* o_sm = reinterpret_cast<float*>(qa_smem + kQaWarps * kStages * Tile::kBytes);  // [warp][8][HD]
+    float2* ml_sm = reinterpret_cast<float2*>(o_sm + kQaWarps * 8 * HD);                  // [warp][rows]
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    uint8_t* ring = ring_all + warp * kStages * Tile::kBytes;
+    wait_for_prior_kernels();
+    long long unused;
+    const long long total = qa_total<kRows>(p, 0, unused), share = qa_share(total, p.blocks);
+    const long long begin = blockIdx.x * share, end = min(begin + share, total);
+    if (begin >= end) return;
+
+    QaCursor cur = qa_locate<kRows>(p, begin), ahead = cur;
+    qa_advance<kRows>(p, ahead, warp);
+    // the producer side of this warp: tiles begin + warp, + kQaWarps, ...
+    long long next = begin + warp;
+    uint32_t valid = 0;  // bit per stage: the tile was found
+    const int table_pages = p.max_pages;
+    auto page_of = [&](const QaCursor& c) {
+        return c.seq < p.n_seq ? __ldg(p.block_table + (size_t)c.seq * table_pages + c.tile / p.page_tiles) : -1;
+    };
+    int page = next < end ? page_of(ahead) : -1;
+    auto fetch = [&](int stage) {
+        valid &= ~(1u << stage);
+        if (next < end) {
+            if ((uint32_t)page < (uint32_t)p.n_pages) {
+                const int head = ahead.item / ahead.q.row_blocks;
+                const char* src = p.cache + (((size_t)page * p.n_heads + head) * p.page_tiles + ahead.tile % p.page_tiles) * Tile::kBytes;
+                uint8_t* dst = ring + stage * Tile::kBytes;
+#pragma unroll
+                for (int i = 0; i < Tile::kBytes / 16; i += 32)
+                    if (i + lane < Tile::kBytes / 16) cp_async16(dst + (i + lane) * 16, src + (i + lane) * 16);
+                valid |= 1u << stage;
+            } else if (p.check && lane == 0) {
+                report_bad_index(p.check, kIndexBadPage, ahead.seq, ahead.tile / p.page_tiles, page);
+            }
+            next += kQaWarps;
+            if (next < end) {
+                qa_advance<kRows>(p, ahead, kQaWarps);
+                page = page_of(ahead);  // used one tile later
+            }
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int st = 0; st < kStages; ++st) fetch(st);
+
+    QaWarp<T, HD, BITS, NT> w;
+    long long at = begin, mine = begin + warp;
+    int stage = 0;
+    while (at < end) {
+        // one item's tiles inside this block's share: [at, to)
+        const long long item_end = at + (cur.q.tiles - cur.tile), to = min(end, item_end);
+        w.begin(p, cur);
+        int sees_all = w.limit[0][0];  // tokens that every column of the warp sees
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sees_all = min(sees_all, min(w.limit[nt][0], w.limit[nt][1]));
+#pragma unroll
+        for (int d = 1; d < 4; d <<= 1) sees_all = min(sees_all, __shfl_xor_sync(0xFFFFFFFFu, sees_all, d));
+        for (; mine < to; mine += kQaWarps) {
+            cp_async_wait<kStages - 1>();
+            __syncwarp();
+            if ((valid >> stage) & 1) {
+                const int pos = (cur.tile + (int)(mine - at)) * kQuantTile;
+                const uint8_t* tile = ring + stage * Tile::kBytes;
+                if (pos + kQuantTile <= sees_all) w.template step<false>(tile, pos);
+                else w.template step<true>(tile, pos);
+            }
+            __syncwarp();
+            fetch(stage);
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+        }
+        // ---- join the warps
+        w.finish();
+        const int g = lane >> 2, t = lane & 3;
+        const int head = cur.item / cur.q.row_blocks, row0 = (cur.item - head * cur.q.row_blocks) * kRows;
+        const int rows = min(kRows, cur.q.q_len * p.group - row0);
+        const bool whole = cur.tile == 0 && to == item_end;
+        float* slot = p.partial + (size_t)(2 * blockIdx.x + (cur.tile > 0 ? 0 : 1)) * kRows * (HD + 2);
+        if (g == 0)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) ml_sm[warp * kRows + nt * 8 + 2 * t + b] = make_float2(w.ref[nt][b], w.l[nt][b]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < HD / 32; ++j)
+                    *reinterpret_cast<float4*>(o_sm + (warp * 8 + 2 * t + b) * HD + j * 32 + g * 4) = w.output(nt, b, j);
+            __syncthreads();
+            for (int i = threadIdx.x; i < 8 * HD / 4; i += kQaThreads) {
+                const int col = i / (HD / 4), ch = (i - col * (HD / 4)) * 4, row = nt * 8 + col;
+                if (row >= rows) continue;
+                float m = kQaNoMax, l = 0.f;
+#pragma unroll
+                for (int k = 0; k < kQaWarps; ++k) m = fmaxf(m, ml_sm[k * kRows + row].x);
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int k = 0; k < kQaWarps; ++k) {
+                    const float2 ml = ml_sm[k * kRows + row];
+                    const float f = exp2_fast(ml.x - m);
+                    const float4 x = *reinterpret_cast<const float4*>(o_sm + (k * 8 + col) * HD + ch);
+                    l = fmaf(ml.y, f, l);
+                    o.x = fmaf(x.x, f, o.x);
+                    o.y = fmaf(x.y, f, o.y);
+                    o.z = fmaf(x.z, f, o.z);
+                    o.w = fmaf(x.w, f, o.w);
+                }
+                if (whole) {
+                    qa_store<T>(p, cur.seq, head, row0 + row, ch, HD, o, m, l);
+                } else {
+                    float* at_row = slot + row * (HD + 2);
+                    *reinterpret_cast<float2*>(at_row + 2 + ch) = make_float2(o.x, o.y);
+                    *reinterpret_cast<float2*>(at_row + 4 + ch) = make_float2(o.z, o.w);
+                    if (ch == 0) *reinterpret_cast<float2*>(at_row) = make_float2(m, l);
+                }
+            }
+            __syncthreads();
+        }
+        const int taken = (int)(to - at);
+        at = to;
+        if (at < end) qa_advance<kRows>(p, cur, taken);
+    }
+}
+
+// Joins the partial results of items that several blocks shared; writes the rows of sequences without
+// tokens.  grid (heads * row blocks, n_seq), HD / 4 threads for each of the rows.
+template <typename T, int HD, int NT>
+__global__ void __launch_bounds__(HD / 4 * 8) quant_attention_join_kernel(const __grid_constant__ QuantAttnParams p)
+{
+    constexpr int kRows = 8 * NT;
+    wait_for_prior_kernels();
+    const int seq = blockIdx.y;
+    const QaSeq q = qa_sequence<kRows>(p, seq);
+    if ((int)blockIdx.x >= q.row_blocks * p.n_heads) return;
+    const int head = blockIdx.x / q.row_blocks, row0 = (blockIdx.x - head * q.row_blocks) * kRows;
+    const int rows = min(kRows, q.q_len * p.group - row0);
+    const int ch = threadIdx.x % (HD / 4) * 4;
+    long long first = 0, last = -1, before;
+    if (q.tiles > 0) {
+        const long long total = qa_total<kRows>(p, seq, before), share = qa_share(total, p.blocks);
+        const long long unit = before + (long long)blockIdx.x * q.tiles;
+        first = unit / share;
+        last = (unit + q.tiles - 1) / share;
+        if (first == last) return;  // written by its block
+    }
+    for (int row = threadIdx.x / (HD / 4); row < rows; row += 8) {
+        float m = kQaNoMax, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (long long b = first; b <= last; ++b) {
+            const float* x = p.partial + ((size_t)(2 * b + (b == first ? 1 : 0)) * kRows + row) * (HD + 2);
+            const float2 ml = *reinterpret_cast<const float2*>(x);
+            const float2 lo = *reinterpret_cast<const float2*>(x + 2 + ch), hi = *reinterpret_cast<const float2*>(x + 4 + ch);
+            const float top = fmaxf(m, ml.x), f0 = exp2_fast(m - top), f1 = exp2_fast(ml.x - top);
+            m = top;
+            l = l * f0 + ml.y * f1;
+            o = make_float4(o.x * f0 + lo.x * f1, o.y * f0 + lo.y * f1, o.z * f0 + hi.x * f1, o.w * f0 + hi.y * f1);
+        }
+        qa_store<T>(p, seq, head, row0 + row, ch, HD, o, m, l);
+    }
+}
+
+}  // namespace civic

@@ -1,0 +1,390 @@
+// The quantised K/V cache: its layout, and the kernels that write rows into it and read them back.
+//
+// A group is 32 consecutive channels of one row (a token's K or V of one head).  With L = 2^bits - 1:
+//     m = min x,   s = (max x - m) / L rounded UP to the payload type T,   code = floor((x - m) / s + 1/2)
+// and the cache stands for s * code + m.  Rounding s up keeps every code within [0, L] without a
+// clamp, so no value is off by more than s / 2; m is exact because it is one of the inputs.
+//
+// A cache page holds [n_heads][page_size / 16] tiles.  A tile is 16 tokens of one K/V head:
+//     K codes | V codes | K parameters | V parameters          (parameters: [16 tokens][groups] {s, m})
+// with the codes in the order in which the attention's matrix instructions take them (QuantTile
+// below), so that attention moves whole 16-byte vectors and never shuffles.  K and V of a tile lie
+// together because attention needs both: one tile is one contiguous piece of 1.25 to 9 KB.
+//
+// Both kernels move bytes (writing reads 2 bytes a channel and writes 0.6 or 1.1); a warp takes one
+// tile of K or of V.  Lanes hold 8 channels of a pair of tokens: four lanes make a group, so minimum
+// and maximum take two shuffles, and a lane's 8 codes are whole words of the layout.
+#pragma once
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "index_check.cuh"
+#include "pdl.cuh"
+
+namespace civic {
+
+constexpr int kQuantTile = 16;     // tokens per tile
+constexpr int kQuantGroup = 32;    // channels per scale
+constexpr int kMaxQuantLayers = 80;
+constexpr int kQuantThreads = 256;
+
+// Layout of a tile, in 32-bit words of codes (8 codes in 4 bits, 4 in 8 bits).
+//   K: lane t of four holds, of every token row, the channels 32 j + 8 t .. + 7 of each group j
+//      (word j; in 8 bits words 2 j and 2 j + 1).  A lane's words of a row lie together, at most four
+//      (16 bytes) to a plane: [plane][row][t][word].
+//   V: lane (g, t) = 4 g + t of a warp holds, for half h of the tile, the tokens 8 h + 2 t and
+//      8 h + 2 t + 1 and of each group j the channels 32 j + 4 g .. + 3.  The low half of a word belongs
+//      to the first token, the high half to the second: [half][plane][lane][word].
+template <int HD, int BITS>
+struct QuantTile {
+    static constexpr int kGroups = HD / kQuantGroup;
+    static constexpr int kWords = kGroups * BITS / 4;  // per lane and row (K), per lane and half (V)
+    static constexpr int kPlane = kWords < 4 ? kWords : 4;
+    static constexpr int kPlanes = kWords / kPlane;
+    static constexpr int kCodeBytes = kQuantTile * HD * BITS / 8;
+    static constexpr int kParamBytes = kQuantTile * kGroups * 4;
+    static constexpr int kVCodes = kCodeBytes;
+    static constexpr int kKParams = 2 * kCodeBytes;
+    static constexpr int kVParams = 2 * kCodeBytes + kParamBytes;
+    static constexpr int kBytes = 2 * (kCodeBytes + kParamBytes);
+    __device__ static constexpr int k_word(int row, int t, int w)
+    {
+        return (((w / kPlane) * kQuantTile + row) * 4 + t) * kPlane + w % kPlane;
+    }
+    __device__ static constexpr int v_word(int half, int lane, int w)
+    {
+        return ((half * kPlanes + w / kPlane) * 32 + lane) * kPlane + w % kPlane;
+    }
+};
+
+inline constexpr int quant_tile_bytes(int head_dim, int bits)
+{
+    return 2 * (kQuantTile * head_dim * bits / 8 + kQuantTile * (head_dim / kQuantGroup) * 4);
+}
+
+struct QuantMoveParams {
+    char* wide[2 * kMaxQuantLayers];   // K, V of every layer: rows of T, read (write kernel) or written (read kernel)
+    char* cache[kMaxQuantLayers];
+    const int32_t* idx;                // [n_seq, n_rows] source rows, or NULL = row j is row j (write kernel)
+    const int32_t* start;              // [n_seq] cache position of row 0, or NULL = 0
+    const int32_t* counts;             // [n_seq] rows of the sequence, or NULL = n_rows
+    const int32_t* block_table;        // [n_seq, max_pages]
+    int64_t seq_stride, token_stride, head_stride;  // of the wide rows, in bytes
+    uint32_t n_units;                  // n_seq * tiles * n_heads
+    int32_t n_heads, tiles;            // tiles a sequence's rows can touch
+    int32_t n_rows, wide_rows;         // rows per sequence at most; valid range of idx
+    int32_t page_tiles, max_pages, n_pages;
+    int32_t* check;                    // fault record or NULL
+};
+
+// ---- 16-bit payload types ------------------------------------------------------------------------
+
+template <typename T>
+struct Half16;
+template <>
+struct Half16<__nv_bfloat16> {
+    __device__ static uint32_t min2(uint32_t a, uint32_t b)
+    {
+        uint32_t d;
+        asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    __device__ static uint32_t max2(uint32_t a, uint32_t b)
+    {
+        uint32_t d;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    __device__ static float lo(uint32_t w) { return __uint_as_float(w << 16); }
+    __device__ static float hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+    __device__ static uint32_t pack(float lo, float hi)
+    {
+        uint32_t d;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+        return d;
+    }
+    // The least bf16 whose `top`-fold is not below range (0 where that has no normal reciprocal), from
+    // q = range / top or slightly less: cut to bf16 it is that number or the one below it, which the
+    // exact product top * s (8 + 8 bits) tells apart.
+    __device__ static uint32_t scale_bits(float range, float q, float top)
+    {
+        uint32_t u = __float_as_uint(q) >> 16;
+        if (__fmul_rn(top, __uint_as_float(u << 16)) < range) ++u;
+        return u < 0x80u ? 0u : u;
+    }
+    static constexpr uint32_t kNan = 0x7FC0u;
+};
+template <>
+struct Half16<__half> {
+    __device__ static uint32_t min2(uint32_t a, uint32_t b)
+    {
+        uint32_t d;
+        asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    __device__ static uint32_t max2(uint32_t a, uint32_t b)
+    {
+        uint32_t d;
+        asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    __device__ static float lo(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)w)); }
+    __device__ static float hi(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
+    __device__ static uint32_t pack(float lo, float hi)
+    {
+        uint32_t d;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+        return d;
+    }
+    __device__ static uint32_t scale_bits(float range, float q, float top)
+    {
+        uint32_t u = __half_as_ushort(__float2half_rz(q));
+        if (__fmul_rn(top, lo(u)) < range) ++u;
+        return u;
+    }
+    static constexpr uint32_t kNan = 0x7E00u;
+};
+
+// ---- one row's 8 channels of a lane ----------------------------------------------------------------
+
+struct Codes8 {
+    uint32_t w[2];   // 8 bits: 4 codes each; 4 bits: w[0] holds all eight
+    uint32_t param;  // {s, m} of the lane's group
+};
+
+// Quantises the lane's 8 channels; its group is the aligned quad of lanes it belongs to.
+template <typename T, int BITS>
+__device__ __forceinline__ Codes8 quantise8(const uint4& v)
+{
+    using H = Half16<T>;
+    constexpr float kTop = BITS == 4 ? 15.f : 255.f;
+    constexpr float kInvTop = BITS == 4 ? 0x1.111110p-4f : 0x1.010100p-8f;  // 1 / L rounded down
+    uint32_t mn = H::min2(H::min2(v.x, v.y), H::min2(v.z, v.w));
+    uint32_t mx = H::max2(H::max2(v.x, v.y), H::max2(v.z, v.w));
+    mn = H::min2(mn, __byte_perm(mn, mn, 0x1032));
+    mx = H::max2(mx, __byte_perm(mx, mx, 0x1032));
+    uint32_t both = __byte_perm(mn, mx ^ 0x80008000u, 0x5410);  // {min, -max}: one minimum reduces both
+    both = H::min2(both, __shfl_xor_sync(0xFFFFFFFFu, both, 1));
+    both = H::min2(both, __shfl_xor_sync(0xFFFFFFFFu, both, 2));
+    const float low = H::lo(both), range = -H::hi(both) - low;
+    const bool finite = range <= 3.402823466e38f;  // false for NaN too
+    const uint32_t sb = finite ? H::scale_bits(range, range * kInvTop, kTop) : H::kNan;
+    Codes8 r;
+    r.param = finite ? (__byte_perm(both, sb, 0x1054)) : (H::kNan * 0x10001u);
+    const float s = H::lo(sb);
+    // 1 / s, never below it: the approximation is within one unit in the last place, one is added.  A
+    // quotient that lies on the border between two codes therefore takes the upper one, as floor(. + 1/2) does.
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    inv = s > 0.f ? __uint_as_float(__float_as_uint(inv) + 1u) : 0.f;
+    const float base = low - 0.5f * s;  // the 1/2 of the rounding
+    auto code = [&](float x) { return __float_as_uint(__fmaf_rd(x - base, inv, 8388608.f)); };  // floor in the low bits
+    const uint32_t c0 = code(H::lo(v.x)), c1 = code(H::hi(v.x)), c2 = code(H::lo(v.y)), c3 = code(H::hi(v.y));
+    const uint32_t c4 = code(H::lo(v.z)), c5 = code(H::hi(v.z)), c6 = code(H::lo(v.w)), c7 = code(H::hi(v.w));
+    if constexpr (BITS == 4) {
+        const uint32_t b01 = __byte_perm(c0 + c1 * 16u, c2 + c3 * 16u, 0x0040);
+        const uint32_t b23 = __byte_perm(c4 + c5 * 16u, c6 + c7 * 16u, 0x0040);
+        r.w[0] = __byte_perm(b01, b23, 0x5410);
+        r.w[1] = 0;
+    } else {
+        r.w[0] = __byte_perm(__byte_perm(c0, c1, 0x0040), __byte_perm(c2, c3, 0x0040), 0x5410);
+        r.w[1] = __byte_perm(__byte_perm(c4, c5, 0x0040), __byte_perm(c6, c7, 0x0040), 0x5410);
+    }
+    return r;
+}
+
+// The values of 8 codes, rounded to T.
+template <typename T, int BITS>
+__device__ __forceinline__ uint4 values8(const Codes8& c)
+{
+    using H = Half16<T>;
+    const float s = H::lo(c.param), m = H::hi(c.param);
+    // s * code is exact (at most 11 + 8 bits), so the sum is rounded once
+    auto value = [&](int i) {
+        const uint32_t w = BITS == 4 ? c.w[0] >> (4 * i) : c.w[i >> 2] >> (8 * (i & 3));
+        const float code = __uint_as_float((w & (BITS == 4 ? 15u : 255u)) | 0x4B000000u) - 8388608.f;
+        return fmaf(s, code, m);
+    };
+    return make_uint4(H::pack(value(0), value(1)), H::pack(value(2), value(3)), H::pack(value(4), value(5)),
+                      H::pack(value(6), value(7)));
+}
+
+// ---- the kernels -----------------------------------------------------------------------------------
+
+// What a warp works on: a tile of the cache, and which rows of the call fall into it.
+struct QuantUnit {
+    int seq, head;
+    char* tile;          // NULL: nothing to do
+    int first;           // call's row number of the tile's token 0 (may be negative)
+    int count;           // the sequence's rows
+};
+
+template <int HD, int BITS>
+__device__ __forceinline__ QuantUnit locate_unit(const QuantMoveParams& p, uint32_t unit, int layer)
+{
+    QuantUnit u;
+    const uint32_t rest = unit / (uint32_t)p.n_heads;
+    u.head = (int)(unit - rest * p.n_heads);
+    u.seq = (int)(rest / (uint32_t)p.tiles);
+    const int tile = (int)(rest - (uint32_t)u.seq * p.tiles);
+    u.tile = nullptr;
+    const int start = p.start ? __ldg(p.start + u.seq) : 0;
+    u.count = p.counts ? min(__ldg(p.counts + u.seq), p.n_rows) : p.n_rows;
+    const long long pos = ((long long)(start >> 4) + tile) * kQuantTile;
+    u.first = (int)(pos - start);
+    if (u.first >= u.count || u.count <= 0) return u;  // no row of the call in this tile
+    const long long page_slot = pos / kQuantTile / p.page_tiles;
+    int page = -1;
+    if (start >= 0 && page_slot < p.max_pages) page = __ldg(p.block_table + (size_t)u.seq * p.max_pages + page_slot);
+    if ((uint32_t)page >= (uint32_t)p.n_pages) {  // neither read nor written
+        if (p.check && (threadIdx.x & 31) == 0) report_bad_index(p.check, kIndexBadPage, u.seq, (int)page_slot, page);
+        return u;
+    }
+    const int sub = (int)(pos / kQuantTile - page_slot * p.page_tiles);
+    u.tile = p.cache[layer] + (((size_t)page * p.n_heads + u.head) * p.page_tiles + sub) * QuantTile<HD, BITS>::kBytes;
+    return u;
+}
+
+// Rows -> cache.  grid (units / 8, 2 * layers), one warp per (sequence, tile, head) and K or V.
+template <typename T, int HD, int BITS>
+__global__ void __launch_bounds__(kQuantThreads) quant_write_kernel(const __grid_constant__ QuantMoveParams p)
+{
+    using Tile = QuantTile<HD, BITS>;
+    constexpr int kLanesPerRow = HD / 8, kPairs = 8 * kLanesPerRow / 32;  // token pairs per lane
+    constexpr int kChunk = kPairs < 4 ? kPairs : 4;                       // of which this many are in flight
+    wait_for_prior_kernels();
+    const int lane = threadIdx.x & 31;
+    const uint32_t unit = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    if (unit >= p.n_units) return;
+    const int layer = blockIdx.y >> 1, is_v = blockIdx.y & 1;
+    const QuantUnit u = locate_unit<HD, BITS>(p, unit, layer);
+    if (!u.tile) return;
+    // source rows: lane r looks up row r of the tile
+    const int j = u.first + (lane & 15);
+    int row = -1;
+    if (j >= 0 && j < u.count) {
+        row = p.idx ? __ldg(p.idx + (size_t)u.seq * p.n_rows + j) : j;
+        if ((uint32_t)row >= (uint32_t)p.wide_rows) {
+            if (p.check && lane < 16) report_bad_index(p.check, kIndexOutOfRange, u.seq, j, row);
+            row = -1;
+        }
+    }
+    const int sub = lane / kLanesPerRow, c = lane % kLanesPerRow, group = c >> 2, quad = c & 3;
+    const char* src = p.wide[blockIdx.y] + u.seq * p.seq_stride + u.head * p.head_stride + c * 16;
+    uint32_t* codes = reinterpret_cast<uint32_t*>(u.tile + (is_v ? Tile::kVCodes : 0));
+    uint32_t* params = reinterpret_cast<uint32_t*>(u.tile + (is_v ? Tile::kVParams : Tile::kKParams));
+#pragma unroll
+    for (int i0 = 0; i0 < kPairs; i0 += kChunk) {
+        uint4 x[kChunk][2];
+        int r[kChunk][2];
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int token = 2 * ((i0 + i) * (8 / kPairs) + sub) + b;
+                r[i][b] = __shfl_sync(0xFFFFFFFFu, row, token);
+                x[i][b] = make_uint4(0, 0, 0, 0);
+                if (r[i][b] >= 0) x[i][b] = __ldcs(reinterpret_cast<const uint4*>(src + r[i][b] * p.token_stride));
+            }
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            const int pair = (i0 + i) * (8 / kPairs) + sub;
+            Codes8 q[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                q[b] = quantise8<T, BITS>(x[i][b]);
+                if (r[i][b] < 0) continue;
+                if (quad == 0) params[(2 * pair + b) * Tile::kGroups + group] = q[b].param;
+                if (!is_v) {
+                    uint32_t* at = codes + Tile::k_word(2 * pair + b, quad, group * (BITS / 4));
+                    if constexpr (BITS == 4) *at = q[b].w[0];
+                    else *reinterpret_cast<uint2*>(at) = make_uint2(q[b].w[0], q[b].w[1]);
+                }
+            }
+            if (is_v) {
+                // channels 8 quad + 0..3 belong to g = 2 quad, 4..7 to g = 2 quad + 1
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int vl = (2 * quad + e) * 4 + (pair & 3);
+#pragma unroll
+                    for (int h = 0; h < BITS / 4; ++h) {
+                        uint32_t* at = codes + Tile::v_word(pair >> 2, vl, group * (BITS / 4) + h);
+                        const uint32_t wa = q[0].w[BITS == 4 ? 0 : e], wb = q[1].w[BITS == 4 ? 0 : e];
+                        const uint32_t w = __byte_perm(wa, wb, (BITS == 4 ? e : h) ? 0x7632 : 0x5410);
+                        if (r[i][0] >= 0 && r[i][1] >= 0) *at = w;
+                        else if (r[i][0] >= 0) *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
+                        else if (r[i][1] >= 0) *(reinterpret_cast<uint16_t*>(at) + 1) = (uint16_t)(w >> 16);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// Cache -> rows, with the same split.  Rows at and behind a sequence's count are left as they were.
+template <typename T, int HD, int BITS>
+__global__ void __launch_bounds__(kQuantThreads) quant_read_kernel(const __grid_constant__ QuantMoveParams p)
+{
+    using Tile = QuantTile<HD, BITS>;
+    constexpr int kLanesPerRow = HD / 8, kPairs = 8 * kLanesPerRow / 32;
+    constexpr int kChunk = kPairs < 4 ? kPairs : 4;
+    wait_for_prior_kernels();
+    const int lane = threadIdx.x & 31;
+    const uint32_t unit = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    if (unit >= p.n_units) return;
+    const int layer = blockIdx.y >> 1, is_v = blockIdx.y & 1;
+    const QuantUnit u = locate_unit<HD, BITS>(p, unit, layer);
+    if (!u.tile) return;
+    const int sub = lane / kLanesPerRow, c = lane % kLanesPerRow, group = c >> 2, quad = c & 3;
+    char* dst = p.wide[blockIdx.y] + u.seq * p.seq_stride + u.head * p.head_stride + c * 16;
+    const uint32_t* codes = reinterpret_cast<const uint32_t*>(u.tile + (is_v ? Tile::kVCodes : 0));
+    const uint32_t* params = reinterpret_cast<const uint32_t*>(u.tile + (is_v ? Tile::kVParams : Tile::kKParams));
+#pragma unroll
+    for (int i0 = 0; i0 < kPairs; i0 += kChunk) {
+        Codes8 q[kChunk][2];
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) {
+            const int pair = (i0 + i) * (8 / kPairs) + sub;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                q[i][b].param = params[(2 * pair + b) * Tile::kGroups + group];
+                if (!is_v) {
+                    const uint32_t* at = codes + Tile::k_word(2 * pair + b, quad, group * (BITS / 4));
+                    q[i][b].w[0] = at[0];
+                    q[i][b].w[1] = BITS == 4 ? 0u : at[BITS / 4 - 1];
+                }
+            }
+            if (is_v) {
+                uint32_t w[2][BITS / 4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int h = 0; h < BITS / 4; ++h)
+                        w[e][h] = codes[Tile::v_word(pair >> 2, (2 * quad + e) * 4 + (pair & 3), group * (BITS / 4) + h)];
+                if constexpr (BITS == 4) {
+                    q[i][0].w[0] = __byte_perm(w[0][0], w[1][0], 0x5410);
+                    q[i][1].w[0] = __byte_perm(w[0][0], w[1][0], 0x7632);
+                    q[i][0].w[1] = q[i][1].w[1] = 0;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        q[i][0].w[e] = __byte_perm(w[e][0], w[e][BITS / 4 - 1], 0x5410);
+                        q[i][1].w[e] = __byte_perm(w[e][0], w[e][BITS / 4 - 1], 0x7632);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int row = u.first + 2 * ((i0 + i) * (8 / kPairs) + sub) + b;
+                if (row >= 0 && row < u.count)
+                    __stcs(reinterpret_cast<uint4*>(dst + row * p.token_stride), values8<T, BITS>(q[i][b]));
+            }
+    }
+}
+
+}  // namespace civic

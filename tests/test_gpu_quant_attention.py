@@ -1,0 +1,375 @@
+"""Attention over the quantised cache, on the GPU, against softmax in 64 bits over the same cache."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import quant_cache as oq
+from paper_2605_28115_b200 import build, civic
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    build.build()
+    civic.load()
+
+
+class Setup:
+    """A cache with `lens` tokens per sequence; what no token wrote is NaN parameters, and table
+    entries behind a sequence's last page are garbage."""
+
+    def __init__(self, lens, heads, dim, bits, page, dtype, seed=0, n_pages=None, k_scale=1.0, edit=None, spare=0):
+        gen = torch.Generator().manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        self.lens_host, self.dtype, self.dim = lens, dtype, dim
+        n_seq, most = len(lens), max(max(lens), 1)
+        per = -(-most // page) + spare
+        self.cache = civic.quant_cache(1, n_pages or n_seq * per + 3, heads, dim, page, bits, dtype, DEV)
+        if n_pages is None:
+            self.cache.buffer.fill_(0xFF)
+        total = self.cache.n_pages
+        pick = total - 1 - rng.permutation(min(total, n_seq * per + 3))[: n_seq * per]
+        self.table_host = pick.reshape(n_seq, per).astype(np.int32)
+        if n_pages is not None:
+            self.cache.buffer[0, torch.from_numpy(pick).long().to(DEV)] = 0xFF
+        self.k, self.v = (torch.randn((n_seq, most, heads, dim), generator=gen) for _ in "kv")
+        self.k[..., 5] *= 6
+        self.k *= k_scale
+        if edit:
+            edit(self.k, self.v)
+        self.k, self.v = self.k.to(dtype), self.v.to(dtype)
+        self.lens = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        table = torch.from_numpy(self.table_host.copy()).to(DEV)
+        civic.civic_append_kv_quant(self.k[None].to(DEV), self.v[None].to(DEV), torch.zeros_like(self.lens), self.cache, table,
+                                    counts=self.lens)
+        for s, n in enumerate(lens):
+            self.table_host[s, -(-n // page):] = rng.choice([-1, -(2**31), 2**31 - 1, total])
+        self.table = torch.from_numpy(self.table_host).to(DEV)
+        self.gen = gen
+
+    def queries(self, q_len, q_heads, scale=1.0):
+        return (torch.randn((len(self.lens_host), q_len, q_heads, self.dim), generator=self.gen) * scale).to(self.dtype)
+
+    def reader(self):
+        pages = sorted({int(p) for s, n in enumerate(self.lens_host) for p in self.table_host[s, : -(-n // self.cache.page_size)]})
+        small = self.cache.buffer[:, pages].cpu().numpy() if pages else np.zeros((1, 0, 1, 1), np.uint8)
+        remap = {p: i for i, p in enumerate(pages)}
+        read = oq.Cache(small, self.cache.page_size, self.dim, self.cache.bits, self.dtype) if pages else None
+        rows = [[remap[int(p)] for p in self.table_host[s, : -(-n // self.cache.page_size)]] for s, n in enumerate(self.lens_host)]
+        return read, rows
+
+
+def check(setup, q, out, lse, scale, causal, q_lens=None, canary=None, sample=None):
+    """Tolerance of an output element: the rounding to T (eps / 2 of it); P' rounded to fp16 (2^-11 of the
+    weighted sum of s * code, which is the output without the minima), elements of P' below 2^-14 of the
+    largest to 2^-25 (2^-24 of the largest s * code a token); and the scores' error d, which moves each
+    weight by a factor of at most exp(2 d).  A score goes through at most 64 roundings of 2^-23 (32-bit sums
+    that the matrix unit may cut instead of rounding) of partial sums below B = scale * sum |q| (s code + |m|)."""
+    read, rows = setup.reader()
+    eps = torch.finfo(setup.dtype).eps / 2
+    for s, n in enumerate(setup.lens_host):
+        ql = q.shape[1] if q_lens is None else q_lens[s]
+        if canary is not None:
+            assert bool((out[s, ql:] == canary).all()) and bool((lse[s, ql:] == canary).all())
+        if n == 0:
+            assert bool((out[s, :ql] == 0).all()) and bool((lse[s, :ql] == -math.inf).all())
+            continue
+        parts = {w: read.raw(0, w, rows[s], n) for w in "kv"}
+        k, v = (oq.values(*parts[w]) for w in "kv")
+        zero = lambda p: oq.values(p[0] * 0, p[1], p[2])
+        vm, km = zero(parts["v"]), zero(parts["k"])
+        group = q.shape[2] // k.shape[1]
+        pairs = [(i, h) for i in range(ql) for h in range(q.shape[2])]
+        if sample and len(pairs) > sample:
+            pairs = [pairs[i] for i in np.random.default_rng(1).permutation(len(pairs))[:sample]]
+        for i, h in pairs:
+            seen = max(0, min(n, n - ql + i + 1)) if causal else n
+            o, e = out[s, i, h].double(), float(lse[s, i, h])
+            if seen == 0:
+                assert bool((o == 0).all()) and e == -math.inf
+                continue
+            kk, vv, mm, x = k[:seen, h // group], v[:seen, h // group], vm[:seen, h // group], q[s, i, h].double()
+            sc = kk @ x * scale
+            w = torch.softmax(sc, 0)
+            want = w @ vv
+            b = float(((kk - km[:seen, h // group] + km[:seen, h // group].abs()) @ x.abs()).max() * abs(scale))
+            d = 64 * 2.0**-23 * b + 2.0**-20
+            codes = vv - mm
+            tol = eps * want.abs() * 1.01 + 2.0**-11 * (w @ codes) + seen * 2.0**-24 * float(w.max()) * codes.amax(0) \
+                + (math.exp(2 * d) - 1) * vv.abs().amax(0) + torch.finfo(setup.dtype).tiny
+            off = (o - want).abs()
+            assert bool((off <= tol).all()), (s, i, h, float((off / tol).max()))
+            want_lse = float(torch.logsumexp(sc, 0))
+            assert abs(e - want_lse) <= d + 2.0**-22 * (abs(want_lse) + float(sc.abs().max())), (s, i, h, e, want_lse, d)
+
+
+def attend(setup, q, **kw):
+    out, lse = civic.civic_quant_attention(q.to(DEV), setup.cache, 0, setup.table, setup.lens, want_lse=True, **kw)
+    return out.cpu(), lse.cpu()
+
+
+SHAPES = [  # lens, heads, q_heads, dim, bits, page, q_len, dtype
+    ([1], 1, 1, 64, 4, 16, 1, torch.bfloat16),
+    ([0], 2, 4, 128, 4, 16, 1, torch.bfloat16),
+    ([15, 16, 17, 0, 1, 33], 2, 8, 128, 4, 16, 1, torch.bfloat16),
+    ([15, 16, 17, 0, 1, 33], 2, 8, 128, 8, 32, 1, torch.bfloat16),
+    ([129], 8, 32, 128, 4, 16, 1, torch.bfloat16),
+    ([405, 1, 77], 8, 32, 128, 4, 64, 1, torch.float16),
+    ([700, 2, 1999], 2, 14, 64, 8, 48, 5, torch.float16),
+    ([300, 40], 1, 8, 64, 4, 16, 3, torch.bfloat16),
+    ([300, 40], 4, 4, 64, 8, 16, 17, torch.bfloat16),
+    ([513, 0, 250], 1, 5, 256, 4, 32, 1, torch.bfloat16),
+    ([100, 61], 2, 6, 256, 8, 16, 7, torch.float16),
+    ([260, 3], 2, 16, 128, 8, 128, 2, torch.float16),
+    ([200, 90], 2, 10, 128, 4, 16, 40, torch.bfloat16),
+    ([5000], 1, 7, 128, 4, 1024, 1, torch.bfloat16),
+]
+
+
+@pytest.mark.parametrize("case", SHAPES)
+@pytest.mark.parametrize("causal", [True, False])
+def test_against_64_bits(case, causal):
+    lens, heads, q_heads, dim, bits, page, q_len, dtype = case
+    setup = Setup(lens, heads, dim, bits, page, dtype, seed=3)
+    q = setup.queries(q_len, q_heads)
+    out, lse = attend(setup, q, causal=causal)
+    check(setup, q, out, lse, dim**-0.5, causal, sample=150)
+    again, lse2 = attend(setup, q, causal=causal)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_padded_queries_and_rows_that_see_nothing():
+    setup = Setup([40, 3, 100, 0], 2, 128, 4, 16, torch.bfloat16, seed=4)
+    q = setup.queries(6, 8)
+    for q_lens in ([6, 5, 0, 2], [1, 6, 3, 6], [9, -2, 1, 1]):
+        some = torch.tensor(q_lens, dtype=torch.int32, device=DEV)
+        out = torch.full((4, 6, 8, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((4, 6, 8), 7.0, dtype=torch.float32, device=DEV)
+        civic.civic_quant_attention(q.to(DEV), setup.cache, 0, setup.table, setup.lens, q_lens=some, out=out, lse=lse)
+        # sequence 1 has 3 tokens: with 5 or 6 query tokens the first ones see nothing
+        check(setup, q, out.cpu(), lse.cpu(), 128**-0.5, True, q_lens=[min(max(x, 0), 6) for x in q_lens], canary=7.0)
+
+
+def test_tokens_that_are_masked_may_hold_anything():
+    def edit(k, v):
+        k[0, 30:], v[0, 30:] = float("nan"), float("inf")
+
+    setup = Setup([33], 2, 64, 8, 16, torch.bfloat16, seed=5, edit=edit)
+    q = setup.queries(5, 4)
+    out, lse = attend(setup, q)  # query tokens at 28 .. 32
+
+    def same_rows(k, v):
+        k[0], v[0] = setup.k[0, :30].float(), setup.v[0, :30].float()
+
+    clean = Setup([30], 2, 64, 8, 16, torch.bfloat16, seed=5, edit=same_rows)
+    want, want_lse = attend(clean, q[:, :2])
+    assert torch.equal(out[:, :2], want) and torch.equal(lse[:, :2], want_lse)
+    assert bool(torch.isnan(out[:, 2:]).all()) and bool(torch.isnan(lse[:, 2:]).all())
+
+
+def test_nan_in_v_stays_in_its_group():
+    def edit(k, v):
+        v[0, 20, 1, 40] = float("nan")
+
+    setup = Setup([50], 2, 128, 4, 16, torch.bfloat16, seed=6, edit=edit)
+    out, lse = attend(setup, setup.queries(1, 4))
+    assert bool(torch.isnan(out[0, 0, 2:, 32:64]).all()) and bool(torch.isfinite(lse).all())
+    assert int(torch.isnan(out).sum()) == 64
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("kind", ["large_scores", "sink", "tiny_v", "huge_v", "tiny_q", "zero_q", "equal_rows"])
+def test_extreme_ranges(bits, kind):
+    def edit(k, v):
+        if kind == "sink":  # a token without weight whose values are a million times the others'
+            k[:, 3] = -4.0
+            v[:, 3] *= 2.0**30
+        elif kind == "tiny_v":
+            v *= 2.0**-70
+        elif kind == "huge_v":
+            v *= 2.0**70
+        elif kind == "equal_rows":
+            k[:], v[:] = 1.25, -3.5
+
+    setup = Setup([77, 20], 1, 64, bits, 16, torch.bfloat16, seed=7, edit=edit, k_scale=8.0 if kind == "large_scores" else 1.0)
+    scale = {"large_scores": 60.0, "tiny_q": 2.0**-110, "zero_q": 0.0}.get(kind, 1.0)
+    q = setup.queries(2, 3, scale)
+    if kind == "sink":
+        q = q.abs() * 2
+    out, lse = attend(setup, q, scale=2.0**105 if kind == "tiny_q" else None)
+    check(setup, q, out, lse, 2.0**105 if kind == "tiny_q" else 0.125, True)
+
+
+def test_q_slices_scale_and_given_buffers():
+    setup = Setup([120, 64], 2, 128, 4, 32, torch.bfloat16, seed=8)
+    fused = torch.randn((2, 3, 4 + 2 + 2, 128), generator=setup.gen).to(torch.bfloat16)
+    q = fused[:, :, :4]
+    out = torch.empty((2, 3, 4, 128), dtype=torch.bfloat16, device=DEV)
+    ws = torch.full((civic.quant_attention_workspace_bytes(setup.cache, 2, 3, 4),), 0xFF, dtype=torch.uint8, device=DEV)
+    got, lse = civic.civic_quant_attention(fused.to(DEV)[:, :, :4], setup.cache, 0, setup.table, setup.lens, scale=-0.2, out=out,
+                                           workspace=ws)
+    assert got is out and lse is None
+    _, lse = attend(setup, q, scale=-0.2)
+    check(setup, q, out.cpu(), lse, -0.2, True)
+    head_major = q.transpose(1, 2).contiguous().to(DEV).transpose(1, 2)
+    again, _ = civic.civic_quant_attention(head_major, setup.cache, 0, setup.table, setup.lens, scale=-0.2)
+    assert torch.equal(again, out)
+
+
+def test_bad_pages_are_left_out_and_recorded():
+    setup = Setup([100], 2, 128, 4, 16, torch.bfloat16, seed=9)
+    q = setup.queries(1, 8)
+    good = int(setup.table_host[0, 2])
+    for bad in (-1, setup.cache.n_pages, 2**31 - 1):
+        setup.table[0, 2] = bad
+        record = torch.zeros(4, dtype=torch.int32, device=DEV)
+        with civic.index_check(record):
+            out, lse = attend(setup, q, causal=False)
+        assert record.tolist() == [3, 0, 2, bad]
+        read, rows = setup.reader()
+        keep = [t for t in range(100) if not 32 <= t < 48]
+        k, v = (read.rows(0, w, rows[0], 100)[keep] for w in "kv")
+        want, want_lse = oq.attention(q[0], k, v, 128**-0.5, False)
+        # the tolerances of `check` at these sizes come to less
+        assert float((out[0].double() - want).abs().max()) < 0.02 and float((lse[0] - want_lse).abs().max()) < 1e-3
+    setup.table[0, 2] = good
+    out, lse = attend(setup, q)
+    check(setup, q, out, lse, 128**-0.5, True)
+
+
+def test_lengths_beyond_the_table_and_below_zero():
+    setup = Setup([48, 20, 31], 1, 64, 4, 16, torch.bfloat16, seed=10)
+    q = setup.queries(1, 4)
+    want, want_lse = attend(setup, q)
+    setup.lens = torch.tensor([10**9, -3, 31], dtype=torch.int32, device=DEV)
+    out, lse = attend(setup, q)
+    assert torch.equal(out[0], want[0]) and torch.equal(lse[0], want_lse[0]) and torch.equal(out[2], want[2])
+    assert bool((out[1] == 0).all()) and bool((lse[1] == -math.inf).all())
+
+
+def test_pages_beyond_four_gigabytes():
+    per_page = 8 * civic.quant_tile_bytes(128, 4)
+    n_pages = (1 << 32) // per_page + 5000
+    setup = Setup([400, 77], 8, 128, 4, 16, torch.bfloat16, seed=11, n_pages=n_pages)
+    assert int(setup.table_host[0, :25].min()) * per_page > 1 << 32
+    q = setup.queries(1, 32)
+    out, lse = attend(setup, q)
+    check(setup, q, out, lse, 128**-0.5, True, sample=40)
+
+
+def test_many_sequences_share_blocks_evenly():
+    rng = np.random.default_rng(12)
+    lens = [int(x) for x in rng.integers(0, 90, 150)]
+    lens[60] = 2500
+    setup = Setup(lens, 2, 64, 4, 16, torch.bfloat16, seed=12)
+    q = setup.queries(1, 4)
+    out, lse = attend(setup, q)
+    check(setup, q, out, lse, 0.125, True)
+
+
+def test_captured_and_replayed_with_new_lengths():
+    setup = Setup([200, 90], 2, 128, 4, 16, torch.bfloat16, seed=13, spare=1)
+    q = setup.queries(1, 8).to(DEV)
+    out = torch.empty_like(q)
+    ws = torch.empty(civic.quant_attention_workspace_bytes(setup.cache, 2, 1, 8), dtype=torch.uint8, device=DEV)
+    lens = setup.lens.clone()
+    run = lambda: civic.civic_quant_attention(q, setup.cache, 0, setup.table, lens, out=out, workspace=ws)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for now in ([200, 90], [1, 64], [0, 89], [77, 0], [200, 1]):
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        out.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, _ = civic.civic_quant_attention(q, setup.cache, 0, setup.table, lens)
+        assert torch.equal(out, want)
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    setups = [Setup([900, 333], 2, 128, 4, 16, torch.bfloat16, seed=s) for s in (14, 15)]
+    qs = [s.queries(1, 8).to(DEV) for s in setups]
+    want = [civic.civic_quant_attention(q, s.cache, 0, s.table, s.lens)[0] for s, q in zip(setups, qs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in setups]
+    got = []
+    for _ in range(20):
+        for s, q, st in zip(setups, qs, streams):
+            got.append(civic.civic_quant_attention(q, s.cache, 0, s.table, s.lens, stream=st)[0])
+    torch.cuda.synchronize()
+    for i, x in enumerate(got):
+        assert torch.equal(x, want[i % 2])
+
+
+def test_select_compact_append_attend_and_read_together():
+    """The path as a user runs it: choose visual tokens, compact every layer's K/V into the cache, then
+    decode: append a token and attend, layer by layer."""
+    gen = torch.Generator().manual_seed(16)
+    layers, n_seq, heads, q_heads, dim, steps = 2, 3, 2, 8, 128, 20
+    desc = civic.SelectDesc(1, 8, 8, 2, 2, 1, 24)
+    seq_len, text_before = 64 + 13, 5
+    scores = torch.rand((n_seq, 64), generator=gen).to(DEV)
+    keep, idx = civic.civic_select_seq(scores, desc, seq_len, text_before)
+    k, v = (torch.randn((layers, n_seq, seq_len, heads, dim), generator=gen).to(torch.bfloat16).to(DEV) for _ in "kv")
+    cache = civic.quant_cache(layers, 20, heads, dim, 16, 4, device=DEV)
+    table = torch.from_numpy(np.random.default_rng(17).permutation(20)[:12].reshape(3, 4).astype(np.int32)).to(DEV)
+    civic.civic_compact_kv_quant(k, v, idx, cache, table)
+    kept = idx.shape[1]
+    lens = torch.full((n_seq,), kept, dtype=torch.int32, device=DEV)
+    news = []
+    for _ in range(steps):
+        kn, vn = (torch.randn((layers, n_seq, 1, heads, dim), generator=gen).to(torch.bfloat16) for _ in "kv")
+        news.append((kn, vn))
+        civic.civic_append_kv_quant(kn.to(DEV), vn.to(DEV), lens, cache, table)
+        lens += 1
+    rows = []
+    for i, x in enumerate((k, v)):
+        old = torch.stack([x[:, s].cpu()[:, idx[s].cpu().long()] for s in range(n_seq)], 1)
+        rows.append(torch.cat([old] + [new[i] for new in news], 2))
+    dense = [oq.values(*oq.quantise(x, 4)) for x in rows]
+    back = [torch.zeros((layers, n_seq, kept + steps, heads, dim), dtype=torch.bfloat16, device=DEV) for _ in "kv"]
+    civic.civic_read_kv_quant(cache, table, lens, *back)
+    for y, x in zip(back, dense):
+        # a code next to a border may differ by one step, at most a handful of them
+        assert float((y.cpu().double() != x.float().bfloat16().double()).double().mean()) < 1e-4
+    for layer in range(layers):
+        q = torch.randn((n_seq, 1, q_heads, dim), generator=gen).to(torch.bfloat16)
+        out, _ = civic.civic_quant_attention(q.to(DEV), cache, layer, table, lens)
+        for s in range(n_seq):
+            want, _ = oq.attention(q[s], dense[0][layer, s], dense[1][layer, s], dim**-0.5, True)
+            # bf16 rounding and fp16 weights: outputs are averages of about 57 values below 5
+            assert float((out[s].cpu().double() - want).abs().max()) < 2.0**-8 * 2 + 2.0**-11 * 5
+
+
+def test_wrong_shapes_devices_and_types_raise():
+    setup = Setup([20], 2, 128, 4, 16, torch.bfloat16, seed=18)
+    q = setup.queries(1, 4).to(DEV)
+    call = lambda q=q, layer=0, table=setup.table, lens=setup.lens, **kw: civic.civic_quant_attention(
+        q, setup.cache, layer, table, lens, **kw)
+    for kw in (dict(q=q.float()), dict(q=q.cpu()), dict(q=q[..., :64]), dict(q=q.transpose(2, 3)), dict(q=q[0]), dict(layer=1),
+               dict(layer=-1), dict(table=setup.table.long()), dict(table=setup.table[0]), dict(lens=setup.lens.cpu()),
+               dict(lens=setup.lens[:0]), dict(q_lens=setup.lens.float()), dict(out=torch.empty_like(q[:, :0])),
+               dict(out=torch.empty_like(q).float()), dict(lse=torch.empty((1, 1, 3), device=DEV)),
+               dict(lse=torch.empty((1, 1, 4), device=DEV, dtype=torch.float64))):
+        with pytest.raises(ValueError):
+            call(**kw)
+    with pytest.raises(civic.CivicError):
+        call(workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+    with pytest.raises(civic.CivicError):
+        call(q=setup.queries(1, 5).to(DEV))
+    with pytest.raises(civic.CivicError):
+        call(scale=float("nan"))
+    x = torch.zeros((1, 1, 4, 2, 128), dtype=torch.bfloat16, device=DEV)
+    start = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for k, v in ((x.float(), x), (x, x.cpu()), (x[:, :, :2], x), (x[0], x), ([x[0], x[0]], [x[0], x[0]]), (x[..., :64], x[..., :64]),
+                 (x.transpose(3, 4).contiguous().transpose(3, 4), x)):
+        with pytest.raises(ValueError):
+            civic.civic_append_kv_quant(k, v, start, setup.cache, setup.table)
+    with pytest.raises(civic.CivicError):
+        civic.civic_read_kv_quant(setup.cache, setup.table, start, x, x)
