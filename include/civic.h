@@ -564,10 +564,12 @@ civic_status_t civic_read_kv_quant(const void* const* cache, const civic_quant_d
  *             them are left as they were
  * out         dev [n_seq, q_len, q_heads, head_dim] contiguous, written
  * lse         dev fp32 [n_seq, q_len, q_heads] or NULL, written; natural logarithm
- * workspace   dev scratch of civic_quant_attention_workspace_bytes(...) bytes, 256-byte aligned; contents
- *             on entry are irrelevant.  Calls that may overlap on the GPU need separate workspaces
+ * workspace   dev scratch of civic_quant_attention_workspace_bytes(...) bytes, 256-byte aligned (NULL where
+ *             that is 0); contents on entry are irrelevant.  Calls that may overlap on the GPU need
+ *             separate workspaces
  * Weights and codes are multiplied as fp16 with fp32 accumulation, scores, sums and lse are fp32.  V
- * groups' scales are expected within 2^-86 .. 2^89, scores may have any size.  Two launches.
+ * groups' scales are expected within 2^-86 .. 2^89, scores may have any size.  One launch where
+ * max_pages_per_seq * page_size <= 512, two otherwise.
  */
 civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q_strides, const void* cache,
                                      const civic_quant_desc_t* desc, const int32_t* block_table, int32_t max_pages_per_seq,
@@ -575,8 +577,9 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
                                      float scale, int32_t causal, void* out, float* lse, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
-/* Scratch bytes civic_quant_attention needs; 0 if the shape is invalid or unsupported. */
-size_t civic_quant_attention_workspace_bytes(const civic_quant_desc_t* desc, int32_t n_seq, int32_t q_len, int32_t q_heads);
+/* Scratch bytes civic_quant_attention needs; 0 if it needs none or the shape is invalid or unsupported. */
+size_t civic_quant_attention_workspace_bytes(const civic_quant_desc_t* desc, int32_t max_pages_per_seq, int32_t n_seq,
+                                             int32_t q_len, int32_t q_heads);
 
 /*
  * Device-side validation of index arrays.

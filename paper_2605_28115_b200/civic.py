@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -162,7 +163,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.civic_quant_attention.argtypes = [vp, strides, vp, desc, vp, i32, vp, vp, i32, i32, i32, ctypes.c_float, i32, vp, vp,
                                           vp, sz, vp]
     lib.civic_quant_attention.restype = ctypes.c_int
-    lib.civic_quant_attention_workspace_bytes.argtypes = [desc, i32, i32, i32]
+    lib.civic_quant_attention_workspace_bytes.argtypes = [desc, i32, i32, i32, i32]
     lib.civic_quant_attention_workspace_bytes.restype = sz
     _lib = lib
     return lib
@@ -196,6 +197,7 @@ def _device_of(*tensors) -> torch.device:
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # the former without the lazy-init check
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -203,7 +205,7 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     if stream is not None:
         return stream.cuda_stream
     if _raw_stream is not None:  # same value as current_stream().cuda_stream without building a Stream object
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -218,7 +220,7 @@ class _on_device:
         self.ctx = None
 
     def __enter__(self):
-        if torch.cuda.current_device() != self.index:
+        if _current_device() != self.index:
             self.ctx = torch.cuda.device(self.index)
             self.ctx.__enter__()
 
@@ -776,29 +778,38 @@ class QuantCache:
     caller-owned; the format is civic.h's).  `dtype` (bfloat16 or float16) is the type of the rows, of the
     queries and of the outputs."""
 
-    __slots__ = ("buffer", "page_size", "head_dim", "bits", "dtype", "n_layers", "n_pages", "n_heads", "desc", "ptr",
-                 "layer_bytes")
+    __slots__ = ("buffer", "page_size", "head_dim", "bits", "dtype", "n_layers", "n_pages", "n_heads", "device", "desc_ref",
+                 "ptr", "layer_bytes", "_tables")
 
     def __init__(self, buffer: torch.Tensor, page_size: int, head_dim: int, bits: int, dtype: torch.dtype = torch.bfloat16):
-        if dtype not in QUANT_DTYPES:
+        code = QUANT_DTYPES.get(dtype)
+        if code is None:
             raise ValueError("dtype must be torch.bfloat16 or torch.float16")
-        if buffer.dim() != 4:
-            raise ValueError("buffer must be [n_layers, n_pages, n_heads, page bytes]")
-        if not buffer.is_cuda:
-            raise ValueError("buffer must be a CUDA tensor")
+        if buffer.dim() != 4 or not buffer.is_cuda:
+            raise ValueError("buffer must be a CUDA tensor [n_layers, n_pages, n_heads, page bytes]")
         self.ptr = _dev_ptr(buffer, "buffer", torch.uint8)
         self.n_layers, self.n_pages, self.n_heads, per_head = buffer.shape
-        self.desc = QuantDesc(self.n_pages, page_size, self.n_heads, head_dim, bits, QUANT_DTYPES[dtype])
-        self.layer_bytes = self.n_pages * int(load().civic_quant_page_bytes(ctypes.byref(self.desc)))
+        self.desc_ref = ctypes.byref(QuantDesc(self.n_pages, page_size, self.n_heads, head_dim, bits, code))
+        self.layer_bytes = self.n_pages * load().civic_quant_page_bytes(self.desc_ref)
         if self.layer_bytes == 0:
             raise CivicError(5, "QuantCache")
         if self.layer_bytes != self.n_pages * self.n_heads * per_head:
             raise ValueError("buffer's last dimension must be page_size / 16 * quant_tile_bytes(head_dim, bits)")
         self.buffer, self.page_size, self.head_dim, self.bits, self.dtype = buffer, page_size, head_dim, bits, dtype
+        self.device, self._tables = buffer.device, None
 
-    def _table(self) -> ctypes.Array:
-        return (ctypes.c_void_p * self.n_layers)(*range(self.ptr, self.ptr + self.n_layers * self.layer_bytes,
-                                                        self.layer_bytes))
+    def tables(self) -> ctypes.Array:
+        """Host pointer table of the layers."""
+        if self._tables is None:
+            self._tables = _pointer_array(self.n_layers)(*range(self.ptr, self.ptr + self.n_layers * self.layer_bytes,
+                                                                self.layer_bytes))
+        return self._tables
+
+
+@functools.lru_cache(maxsize=None)
+def _pointer_array(n: int):
+    """The ctypes type of n pointers (creating one takes microseconds)."""
+    return ctypes.c_void_p * n
 
 
 def quant_cache(n_layers: int, n_pages: int, n_heads: int, head_dim: int, page_size: int = 16, bits: int = 4,
@@ -813,16 +824,17 @@ def quant_cache(n_layers: int, n_pages: int, n_heads: int, head_dim: int, page_s
 
 def _rows_of(cache: QuantCache, x, what: str):
     """Per-layer row tensors [n_seq, rows, n_heads, head_dim], stacked [n_layers, ...] or as a sequence ->
-    (pointer table, strides, n_seq, rows).  Any strides with a contiguous last dimension, the same for all layers."""
+    (pointer table, (n_seq, rows), strides).  Any strides with a contiguous last dimension, the same for all layers."""
+    n = cache.n_layers
     if isinstance(x, torch.Tensor):
-        if x.dim() != 5 or x.shape[0] != cache.n_layers:
+        if x.dim() != 5 or x.shape[0] != n:
             raise ValueError(f"{what} must be [n_layers, n_seq, rows, n_heads, head_dim]")
         _, n_seq, rows, heads, dim = x.shape
-        per_layer, seq, token, head, last = x.stride()
-        first, base, step = x, x.data_ptr(), per_layer * x.element_size()
-        table = (ctypes.c_void_p * cache.n_layers)(*[base + i * step for i in range(cache.n_layers)])
+        step, seq, token, head, last = x.stride()
+        first, base = x, x.data_ptr()
+        table = _pointer_array(n)(*[base + 2 * i * step for i in range(n)])
     else:
-        if len(x) != cache.n_layers or any(t.dim() != 4 for t in x):
+        if len(x) != n or any(t.dim() != 4 for t in x):
             raise ValueError(f"{what} must be one [n_seq, rows, n_heads, head_dim] tensor per layer of the cache")
         first = x[0]
         if any(t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype or t.device != first.device
@@ -830,28 +842,30 @@ def _rows_of(cache: QuantCache, x, what: str):
             raise ValueError(f"all {what} tensors must share shape, strides, dtype and device")
         n_seq, rows, heads, dim = first.shape
         seq, token, head, last = first.stride()
-        table = (ctypes.c_void_p * cache.n_layers)(*[t.data_ptr() for t in x])
-    if heads != cache.n_heads or dim != cache.head_dim or first.dtype != cache.dtype:
-        raise ValueError(f"{what} must have the cache's {cache.n_heads} heads of {cache.head_dim} in {cache.dtype}")
-    if last != 1:
-        raise ValueError(f"{what}: the last dimension must be contiguous")
-    _on_cache_device(cache, first, what)
-    return table, (seq, token, head), n_seq, rows
+        table = _pointer_array(n)(*[t.data_ptr() for t in x])
+    if heads != cache.n_heads or dim != cache.head_dim or first.dtype is not cache.dtype or last != 1:
+        raise ValueError(f"{what} must have the cache's {cache.n_heads} heads of {cache.head_dim} in {cache.dtype}, "
+                         "the last dimension contiguous")
+    if first.device != cache.device:
+        _need_device(cache, first, what)
+    return table, (n_seq, rows), (seq, token, head)
 
 
-def _on_cache_device(cache: QuantCache, x: torch.Tensor, what: str) -> None:
-    if not (x.device == cache.buffer.device or x.is_pinned()):
-        raise ValueError(f"{what} must be on the cache's device {cache.buffer.device}")
+def _need_device(cache: QuantCache, x: torch.Tensor, what: str) -> None:
+    """Raises unless x, which is not on the cache's device, is pinned host memory."""
+    if x.device != cache.device and not x.is_pinned():
+        raise ValueError(f"{what} must be on the cache's device {cache.device}")
 
 
 def _seq_words(cache: QuantCache, x: Optional[torch.Tensor], n_seq: int, what: str, dims: int = 1) -> Optional[int]:
     """Pointer of an int32 tensor whose first dimension is n_seq."""
     if x is None:
         return None
-    if x.dim() != dims or x.shape[0] != n_seq:
-        raise ValueError(f"{what} must be [n_seq]" if dims == 1 else f"{what} must be [n_seq, ...]")
-    _on_cache_device(cache, x, what)
-    return _dev_ptr(x, what, torch.int32)
+    if x.dtype is not torch.int32 or x.dim() != dims or x.shape[0] != n_seq or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor [n_seq{', ...' if dims > 1 else ''}]")
+    if x.device != cache.device:
+        _need_device(cache, x, what)
+    return x.data_ptr()
 
 
 def civic_compact_kv_quant(k_src, v_src, seq_idx: torch.Tensor, cache: QuantCache, block_table: torch.Tensor,
@@ -859,15 +873,16 @@ def civic_compact_kv_quant(k_src, v_src, seq_idx: torch.Tensor, cache: QuantCach
     """Kept rows of every layer's K and V, quantised, into `cache`: row seq_idx[s, j] becomes token j of sequence s.
     k_src, v_src [n_layers, n_seq, seq_len, n_heads, head_dim] (or a sequence of per-layer tensors) with equal
     strides; seq_idx int32 [n_seq, s_out]; block_table int32 [n_seq, max_pages_per_seq]."""
-    k, strides, n_seq, seq_len = _rows_of(cache, k_src, "k_src")
-    v, v_strides, *v_shape = _rows_of(cache, v_src, "v_src")
-    if v_strides != strides or v_shape != [n_seq, seq_len]:
+    k, shape, strides = _rows_of(cache, k_src, "k_src")
+    v, *same = _rows_of(cache, v_src, "v_src")
+    if same != [shape, strides]:
         raise ValueError("k_src and v_src must share shape and strides")
+    n_seq, seq_len = shape
     idx = _seq_words(cache, seq_idx, n_seq, "seq_idx", 2)
     table = _seq_words(cache, block_table, n_seq, "block_table", 2)
-    with _on_device(cache.buffer.device):
+    with _on_device(cache.device):
         _check(load().civic_compact_kv_quant(k, v, ctypes.byref(RowStrides(*strides)), cache.n_layers, n_seq, seq_len,
-                                             seq_idx.shape[1], idx, cache._table(), ctypes.byref(cache.desc), table,
+                                             seq_idx.shape[1], idx, cache.tables(), cache.desc_ref, table,
                                              block_table.shape[1], _stream_ptr(stream)), "civic_compact_kv_quant")
 
 
@@ -876,16 +891,17 @@ def civic_append_kv_quant(k_new, v_new, start: torch.Tensor, cache: QuantCache, 
     """New tokens' rows into `cache`: row j < counts[s] (default: all) becomes token start[s] + j of sequence s.
     k_new, v_new [n_layers, n_seq, n_new, n_heads, head_dim] (or a sequence of per-layer tensors); start, counts
     int32 [n_seq]; block_table int32 [n_seq, max_pages_per_seq]."""
-    k, strides, n_seq, n_new = _rows_of(cache, k_new, "k_new")
-    v, v_strides, *v_shape = _rows_of(cache, v_new, "v_new")
-    if v_strides != strides or v_shape != [n_seq, n_new]:
+    k, shape, strides = _rows_of(cache, k_new, "k_new")
+    v, *same = _rows_of(cache, v_new, "v_new")
+    if same != [shape, strides]:
         raise ValueError("k_new and v_new must share shape and strides")
+    n_seq, n_new = shape
     at = _seq_words(cache, start, n_seq, "start")
     some = _seq_words(cache, counts, n_seq, "counts")
     table = _seq_words(cache, block_table, n_seq, "block_table", 2)
-    with _on_device(cache.buffer.device):
+    with _on_device(cache.device):
         _check(load().civic_append_kv_quant(k, v, ctypes.byref(RowStrides(*strides)), cache.n_layers, n_seq, n_new, at, some,
-                                            cache._table(), ctypes.byref(cache.desc), table, block_table.shape[1],
+                                            cache.tables(), cache.desc_ref, table, block_table.shape[1],
                                             _stream_ptr(stream)), "civic_append_kv_quant")
 
 
@@ -894,22 +910,24 @@ def civic_read_kv_quant(cache: QuantCache, block_table: torch.Tensor, counts: to
     """Rows of `cache` in its dtype: token start[s] + j (start None: j) of sequence s to row j < counts[s] of k_out and
     v_out [n_layers, n_seq, max_rows, n_heads, head_dim] (or sequences of per-layer tensors); the rows behind are
     left as they were.  counts, start int32 [n_seq].  Returns (k_out, v_out)."""
-    k, strides, n_seq, rows = _rows_of(cache, k_out, "k_out")
-    v, v_strides, *v_shape = _rows_of(cache, v_out, "v_out")
-    if v_strides != strides or v_shape != [n_seq, rows]:
+    k, shape, strides = _rows_of(cache, k_out, "k_out")
+    v, *same = _rows_of(cache, v_out, "v_out")
+    if same != [shape, strides]:
         raise ValueError("k_out and v_out must share shape and strides")
+    n_seq, rows = shape
     some = _seq_words(cache, counts, n_seq, "counts")
     at = _seq_words(cache, start, n_seq, "start")
     table = _seq_words(cache, block_table, n_seq, "block_table", 2)
-    with _on_device(cache.buffer.device):
-        _check(load().civic_read_kv_quant(cache._table(), ctypes.byref(cache.desc), table, block_table.shape[1],
-                                          cache.n_layers, n_seq, rows, at, some, k, v, ctypes.byref(RowStrides(*strides)),
-                                          _stream_ptr(stream)), "civic_read_kv_quant")
+    with _on_device(cache.device):
+        _check(load().civic_read_kv_quant(cache.tables(), cache.desc_ref, table, block_table.shape[1], cache.n_layers, n_seq,
+                                          rows, at, some, k, v, ctypes.byref(RowStrides(*strides)), _stream_ptr(stream)),
+               "civic_read_kv_quant")
     return k_out, v_out
 
 
-def quant_attention_workspace_bytes(cache: QuantCache, n_seq: int, q_len: int, q_heads: int) -> int:
-    return int(load().civic_quant_attention_workspace_bytes(ctypes.byref(cache.desc), n_seq, q_len, q_heads))
+def quant_attention_workspace_bytes(cache: QuantCache, max_pages: int, n_seq: int, q_len: int, q_heads: int) -> int:
+    """Scratch bytes of civic_quant_attention for block tables of max_pages entries a row; 0: none needed."""
+    return int(load().civic_quant_attention_workspace_bytes(cache.desc_ref, max_pages, n_seq, q_len, q_heads))
 
 
 def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_table: torch.Tensor, lens: torch.Tensor,
@@ -921,43 +939,48 @@ def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_
     q [n_seq, q_len, q_heads, head_dim], any strides with a contiguous last dimension; lens int32 [n_seq] tokens in the
     cache, the query tokens among them (causal: they are the last ones); q_lens int32 [n_seq] query tokens of each
     sequence (default: all q_len), rows behind them are left as they were."""
-    if q.dim() != 4 or q.shape[3] != cache.head_dim or q.dtype != cache.dtype or q.stride(3) != 1:
+    n_seq, q_len, q_heads, dim = q.shape if q.dim() == 4 else (0, 0, 0, -1)
+    seq, token, head, last = q.stride() if q.dim() == 4 else (0, 0, 0, -1)
+    if dim != cache.head_dim or q.dtype is not cache.dtype or last != 1:
         raise ValueError(f"q must be [n_seq, q_len, q_heads, {cache.head_dim}] in {cache.dtype}, its last dimension contiguous")
     if not 0 <= layer < cache.n_layers:
         raise ValueError("layer must be one of the cache's")
-    _on_cache_device(cache, q, "q")
-    n_seq, q_len, q_heads, dim = q.shape
-    dev = cache.buffer.device
+    dev = cache.device
+    if q.device != dev:
+        _need_device(cache, q, "q")
     table = _seq_words(cache, block_table, n_seq, "block_table", 2)
     n_tok = _seq_words(cache, lens, n_seq, "lens")
     n_q = _seq_words(cache, q_lens, n_seq, "q_lens")
+    max_pages = block_table.shape[1]
     made = []  # allocated here: not to be handed out again before `stream` is done with it
     if out is None:
-        out = torch.empty((n_seq, q_len, q_heads, dim), dtype=cache.dtype, device=dev)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
         made.append(out)
-    elif tuple(out.shape) != (n_seq, q_len, q_heads, dim):
+    elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
-    if lse is None and want_lse:
-        lse = torch.empty((n_seq, q_len, q_heads), dtype=torch.float32, device=dev)
-        made.append(lse)
-    elif lse is not None and tuple(lse.shape) != (n_seq, q_len, q_heads):
+    if lse is None:
+        if want_lse:
+            lse = out.new_empty((n_seq, q_len, q_heads), dtype=torch.float32)
+            made.append(lse)
+    elif lse.shape != q.shape[:3]:
         raise ValueError("lse must be [n_seq, q_len, q_heads]")
-    need = quant_attention_workspace_bytes(cache, n_seq, q_len, q_heads)
+    lib = load()
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-        made.append(workspace)
-    else:
-        _on_cache_device(cache, workspace, "workspace")
-    seq, token, head, _ = q.stride()
+        need = lib.civic_quant_attention_workspace_bytes(cache.desc_ref, max_pages, n_seq, q_len, q_heads)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+            made.append(workspace)
+    elif workspace.device != dev:
+        _need_device(cache, workspace, "workspace")
     if stream is not None:
         for t in made:
             t.record_stream(stream)
     with _on_device(dev):
-        _check(load().civic_quant_attention(
-            q.data_ptr(), ctypes.byref(RowStrides(seq, token, head)), cache.ptr + layer * cache.layer_bytes,
-            ctypes.byref(cache.desc), table, block_table.shape[1], n_tok, n_q, n_seq, q_len, q_heads,
-            dim ** -0.5 if scale is None else scale, 1 if causal else 0, _dev_ptr(out, "out", cache.dtype),
-            _dev_ptr(lse, "lse", torch.float32), _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel(),
+        _check(lib.civic_quant_attention(
+            q.data_ptr(), ctypes.byref(RowStrides(seq, token, head)), cache.ptr + layer * cache.layer_bytes, cache.desc_ref,
+            table, max_pages, n_tok, n_q, n_seq, q_len, q_heads, dim ** -0.5 if scale is None else scale, causal,
+            _dev_ptr(out, "out", cache.dtype), _dev_ptr(lse, "lse", torch.float32),
+            _dev_ptr(workspace, "workspace", torch.uint8), 0 if workspace is None else workspace.numel(),
             _stream_ptr(stream)), "civic_quant_attention")
     return out, lse
 

@@ -227,9 +227,14 @@ civic_status_t launch_attention(civic::QuantAttnParams& p, unsigned items, cudaS
         if (per_sm < 1) return CIVIC_ERR_UNSUPPORTED;
         if (dev >= 0) resident[dev].store(per_sm, std::memory_order_relaxed);
     }
+    const bool pdl = programmatic();
+    if (p.blocks == 0) {
+        CIVIC_CUDA_TRY(civic::launch(pdl, kernel, dim3(items, (unsigned)p.n_seq), (unsigned)civic::kQaThreads, smem, stream, p));
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+        return CIVIC_OK;
+    }
     const int blocks = sm_count() * per_sm;
     p.blocks = blocks < civic::kQaMaxBlocks ? blocks : civic::kQaMaxBlocks;
-    const bool pdl = programmatic();
     CIVIC_CUDA_TRY(civic::launch(pdl, kernel, (unsigned)p.blocks, (unsigned)civic::kQaThreads, smem, stream, p));
     CIVIC_CUDA_TRY(civic::launch(pdl, civic::quant_attention_join_kernel<T, HD, NT>, dim3(items, (unsigned)p.n_seq),
                                  (unsigned)(HD / 4 * 8), 0, stream, p));
@@ -265,8 +270,15 @@ civic_status_t check_attention(const civic_quant_desc_t* desc, int32_t n_seq, in
     return CIVIC_OK;
 }
 
-size_t attention_workspace(const civic_quant_desc_t& d, int32_t q_len, int32_t q_heads)
+// Whether an item's tiles are few enough for one block.
+bool whole_items(const civic_quant_desc_t& d, int32_t max_pages)
 {
+    return (int64_t)max_pages * d.page_size <= civic::kQaWholeTiles * civic::kQuantTile;
+}
+
+size_t attention_workspace(const civic_quant_desc_t& d, int32_t max_pages, int32_t q_len, int32_t q_heads)
+{
+    if (whole_items(d, max_pages)) return 0;
     const int nt = attention_tiles(d.head_dim, (int64_t)q_len * (q_heads / d.n_heads));
     return round_up((size_t)2 * civic::kQaMaxBlocks * 8 * nt * (d.head_dim + 2) * 4, 256);
 }
@@ -313,9 +325,11 @@ civic_status_t civic_read_kv_quant(const void* const* cache, const civic_quant_d
     return move_impl(c, stream);
 }
 
-size_t civic_quant_attention_workspace_bytes(const civic_quant_desc_t* desc, int32_t n_seq, int32_t q_len, int32_t q_heads)
+size_t civic_quant_attention_workspace_bytes(const civic_quant_desc_t* desc, int32_t max_pages_per_seq, int32_t n_seq,
+                                             int32_t q_len, int32_t q_heads)
 {
-    return check_attention(desc, n_seq, q_len, q_heads) == CIVIC_OK ? attention_workspace(*desc, q_len, q_heads) : 0;
+    if (check_attention(desc, n_seq, q_len, q_heads) != CIVIC_OK || max_pages_per_seq < 0) return 0;
+    return attention_workspace(*desc, max_pages_per_seq, q_len, q_heads);
 }
 
 civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q_strides, const void* cache,
@@ -336,9 +350,11 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     if (!aligned(q, 16) || !aligned(cache, 16) || !aligned(out, 16) || !aligned(block_table, 4) || !aligned(lens, 4) ||
         !aligned(q_lens, 4) || !aligned(lse, 4))
         return CIVIC_ERR_ALIGNMENT;
-    const size_t need = attention_workspace(d, q_len, q_heads);
-    if (!workspace || workspace_bytes < need) return CIVIC_ERR_WORKSPACE;
-    if (!aligned(workspace, 256)) return CIVIC_ERR_ALIGNMENT;
+    const size_t need = attention_workspace(d, max_pages_per_seq, q_len, q_heads);
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need) return CIVIC_ERR_WORKSPACE;
+        if (!aligned(workspace, 256)) return CIVIC_ERR_ALIGNMENT;
+    }
     {
         const size_t rows = (size_t)n_seq * q_len * q_heads;
         const void* made[3] = {out, lse, workspace};
@@ -378,6 +394,7 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     p.capacity = max_pages_per_seq * d.page_size;
     p.scale_log2e = scale * 1.4426950408889634f;
     p.check = g_index_check;
+    p.blocks = whole_items(d, max_pages_per_seq) ? 0 : 1;  // 1: sized to the device below
     const int64_t rows = (int64_t)q_len * p.group;
     const int nt = attention_tiles(d.head_dim, rows);
     const unsigned items = (unsigned)((rows + 8 * nt - 1) / (8 * nt) * d.n_heads);

@@ -26,7 +26,8 @@
 // balance themselves and the lengths stay on the device.  A block's warps take the tiles of its
 // share in turn, each with its own ring of tiles in shared memory that cp.async fills ahead.
 // Shares that cut an item leave partial results (m, l, O) in the workspace, and a second small kernel
-// joins them in a fixed order.
+// joins them in a fixed order.  Where the block tables are short (kQaWholeTiles) a block takes an item as
+// a whole instead: one launch, no workspace.
 #pragma once
 #include "quant_cache.cuh"
 
@@ -36,6 +37,7 @@ constexpr int kQaWarps = 4;
 constexpr int kQaThreads = 32 * kQaWarps;
 constexpr int kQaMaxBlocks = 148 * 4;  // also fixes the workspace size
 constexpr int kQaMinTiles = 2 * kQaWarps;
+constexpr int kQaWholeTiles = 32;      // tables up to this many tiles: a block per item, nothing to join
 constexpr float kQaNoMax = -1e30f;     // reference of a row that has seen nothing
 constexpr float kQaSlack = 8.f;        // P' stays below 2^9
 
@@ -53,7 +55,7 @@ struct QuantAttnParams {
     int32_t causal;
     int32_t page_tiles, max_pages, n_pages;
     int32_t capacity;            // tokens the block table can address
-    int32_t blocks;              // of the main kernel
+    int32_t blocks;              // of the main kernel where items are shared between blocks; 0 = a block per item
     float scale_log2e;
     int32_t* check;
 };
@@ -207,22 +209,33 @@ struct QaWarp {
     float ref[NT][2], l[NT][2], v_min[NT][2][NG];
     float o[NT][MT][4];
 
-    __device__ __forceinline__ void begin(const QuantAttnParams& p, const QaCursor& c)
+    // The item's query rows; only issues the loads.
+    __device__ __forceinline__ static void load_q(const QuantAttnParams& p, const QaCursor& c, uint4 (&x)[NT][NG])
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const int head = c.item / c.q.row_blocks, row0 = (c.item - head * c.q.row_blocks) * (8 * NT);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = row0 + nt * 8 + g, token = row / p.group, sub = row - token * p.group;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                x[nt][j] = make_uint4(0, 0, 0, 0);
+                if (token < p.q_len)  // rows behind a sequence's own q_len are read and not used
+                    x[nt][j] = __ldg(reinterpret_cast<const uint4*>(p.q + c.seq * p.q_seq + token * p.q_token +
+                                                                    (head * p.group + sub) * p.q_head + (j * 32 + t * 8) * 2));
+            }
+        }
+    }
+
+    __device__ __forceinline__ void begin(const QuantAttnParams& p, const QaCursor& c, const uint4 (&xs)[NT][NG])
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         const int head = c.item / c.q.row_blocks, row0 = (c.item - head * c.q.row_blocks) * (8 * NT);
         const int rows = c.q.q_len * p.group;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int row = row0 + nt * 8 + g, token = row / p.group, sub = row - token * p.group;
-            uint4 x[NG];
-#pragma unroll
-            for (int j = 0; j < NG; ++j) {
-                x[j] = make_uint4(0, 0, 0, 0);
-                if (row < rows)
-                    x[j] = __ldg(reinterpret_cast<const uint4*>(p.q + c.seq * p.q_seq + token * p.q_token +
-                                                                (head * p.group + sub) * p.q_head + (j * 32 + t * 8) * 2));
-            }
+            const int row = row0 + nt * 8 + g, token = row / p.group;
+            const uint4(&x)[NG] = xs[nt];
             // the row's power of two
             float top = 0.f;
             float f[NG][8];
@@ -531,22 +544,48 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
     float2* ml_sm = reinterpret_cast<float2*>(o_sm + kQaWarps * 8 * HD);                  // [warp][rows]
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     uint8_t* ring = ring_all + warp * kStages * Tile::kBytes;
+    release_next_kernel();  // the joining kernel is small: its blocks may wait beside this one's
     wait_for_prior_kernels();
-    long long unused;
-    const long long total = qa_total<kRows>(p, 0, unused), share = qa_share(total, p.blocks);
-    const long long begin = blockIdx.x * share, end = min(begin + share, total);
-    if (begin >= end) return;
-
-    QaCursor cur = qa_locate<kRows>(p, begin), ahead = cur;
-    qa_advance<kRows>(p, ahead, warp);
-    // the producer side of this warp: tiles begin + warp, + kQaWarps, ...
-    long long next = begin + warp;
-    uint32_t valid = 0;  // bit per stage: the tile was found
+    QaWarp<T, HD, BITS, NT> w;
+    uint4 x[NT][Tile::kGroups];
+    QaCursor cur, ahead;
+    long long begin, end;
+    int page = -1;  // of this warp's next tile
     const int table_pages = p.max_pages;
     auto page_of = [&](const QaCursor& c) {
         return c.seq < p.n_seq ? __ldg(p.block_table + (size_t)c.seq * table_pages + c.tile / p.page_tiles) : -1;
     };
-    int page = next < end ? page_of(ahead) : -1;
+    if (p.blocks == 0) {
+        // a block per item: the lengths, the first pages and the queries are fetched at once
+        cur.seq = blockIdx.y;
+        cur.item = blockIdx.x;
+        cur.tile = 0;
+        if (warp / p.page_tiles < table_pages) page = __ldg(p.block_table + (size_t)cur.seq * table_pages + warp / p.page_tiles);
+        cur.q.row_blocks = (p.q_len * p.group + kRows - 1) / kRows;  // with q_lens: as many blocks per head as the longest needs
+        w.load_q(p, cur, x);
+        const int row_blocks = cur.q.row_blocks;
+        cur.q = qa_sequence<kRows>(p, cur.seq);
+        if (cur.item % row_blocks >= cur.q.row_blocks) return;
+        cur.q.row_blocks = row_blocks;
+        ahead = cur;
+        ahead.tile = warp;
+        begin = 0;
+        end = cur.q.tiles;
+    } else {
+        long long unused;
+        const long long total = qa_total<kRows>(p, 0, unused), share = qa_share(total, p.blocks);
+        begin = blockIdx.x * share;
+        end = min(begin + share, total);
+        if (begin >= end) return;
+        cur = qa_locate<kRows>(p, begin);
+        ahead = cur;
+        qa_advance<kRows>(p, ahead, warp);
+        if (begin + warp < end) page = page_of(ahead);
+        w.load_q(p, cur, x);
+    }
+    // the producer side of this warp: tiles begin + warp, + kQaWarps, ...
+    long long next = begin + warp;
+    uint32_t valid = 0;  // bit per stage: the tile was found
     auto fetch = [&](int stage) {
         valid &= ~(1u << stage);
         if (next < end) {
@@ -572,13 +611,12 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
 #pragma unroll
     for (int st = 0; st < kStages; ++st) fetch(st);
 
-    QaWarp<T, HD, BITS, NT> w;
     long long at = begin, mine = begin + warp;
     int stage = 0;
-    while (at < end) {
+    do {
         // one item's tiles inside this block's share: [at, to)
         const long long item_end = at + (cur.q.tiles - cur.tile), to = min(end, item_end);
-        w.begin(p, cur);
+        w.begin(p, cur, x);
         int sees_all = w.limit[0][0];  // tokens that every column of the warp sees
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sees_all = min(sees_all, min(w.limit[nt][0], w.limit[nt][1]));
@@ -648,8 +686,11 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
         }
         const int taken = (int)(to - at);
         at = to;
-        if (at < end) qa_advance<kRows>(p, cur, taken);
-    }
+        if (at < end) {
+            qa_advance<kRows>(p, cur, taken);
+            w.load_q(p, cur, x);
+        }
+    } while (at < end);
 }
 
 // Joins the partial results of items that several blocks shared; writes the rows of sequences without

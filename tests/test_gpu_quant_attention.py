@@ -23,6 +23,7 @@ class Setup:
     entries behind a sequence's last page are garbage."""
 
     def __init__(self, lens, heads, dim, bits, page, dtype, seed=0, n_pages=None, k_scale=1.0, edit=None, spare=0):
+        """`spare`: entries of the block table that no length needs."""
         gen = torch.Generator().manual_seed(seed)
         rng = np.random.default_rng(seed)
         self.lens_host, self.dtype, self.dim = lens, dtype, dim
@@ -132,9 +133,10 @@ SHAPES = [  # lens, heads, q_heads, dim, bits, page, q_len, dtype
 
 @pytest.mark.parametrize("case", SHAPES)
 @pytest.mark.parametrize("causal", [True, False])
-def test_against_64_bits(case, causal):
+@pytest.mark.parametrize("spare", [0, 33])  # tables beyond 512 tokens take the kernels that share items between blocks
+def test_against_64_bits(case, causal, spare):
     lens, heads, q_heads, dim, bits, page, q_len, dtype = case
-    setup = Setup(lens, heads, dim, bits, page, dtype, seed=3)
+    setup = Setup(lens, heads, dim, bits, page, dtype, seed=3, spare=spare)
     q = setup.queries(q_len, q_heads)
     out, lse = attend(setup, q, causal=causal)
     check(setup, q, out, lse, dim**-0.5, causal, sample=150)
@@ -142,8 +144,9 @@ def test_against_64_bits(case, causal):
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
-def test_padded_queries_and_rows_that_see_nothing():
-    setup = Setup([40, 3, 100, 0], 2, 128, 4, 16, torch.bfloat16, seed=4)
+@pytest.mark.parametrize("spare", [0, 33])
+def test_padded_queries_and_rows_that_see_nothing(spare):
+    setup = Setup([40, 3, 100, 0], 2, 128, 4, 16, torch.bfloat16, seed=4, spare=spare)
     q = setup.queries(6, 8)
     for q_lens in ([6, 5, 0, 2], [1, 6, 3, 6], [9, -2, 1, 1]):
         some = torch.tensor(q_lens, dtype=torch.int32, device=DEV)
@@ -205,11 +208,11 @@ def test_extreme_ranges(bits, kind):
 
 
 def test_q_slices_scale_and_given_buffers():
-    setup = Setup([120, 64], 2, 128, 4, 32, torch.bfloat16, seed=8)
+    setup = Setup([520, 64], 2, 128, 4, 32, torch.bfloat16, seed=8)
     fused = torch.randn((2, 3, 4 + 2 + 2, 128), generator=setup.gen).to(torch.bfloat16)
     q = fused[:, :, :4]
     out = torch.empty((2, 3, 4, 128), dtype=torch.bfloat16, device=DEV)
-    ws = torch.full((civic.quant_attention_workspace_bytes(setup.cache, 2, 3, 4),), 0xFF, dtype=torch.uint8, device=DEV)
+    ws = torch.full((civic.quant_attention_workspace_bytes(setup.cache, 17, 2, 3, 4),), 0xFF, dtype=torch.uint8, device=DEV)
     got, lse = civic.civic_quant_attention(fused.to(DEV)[:, :, :4], setup.cache, 0, setup.table, setup.lens, scale=-0.2, out=out,
                                            workspace=ws)
     assert got is out and lse is None
@@ -271,11 +274,12 @@ def test_many_sequences_share_blocks_evenly():
     check(setup, q, out, lse, 0.125, True)
 
 
-def test_captured_and_replayed_with_new_lengths():
-    setup = Setup([200, 90], 2, 128, 4, 16, torch.bfloat16, seed=13, spare=1)
+@pytest.mark.parametrize("spare", [0, 20])  # short tables: a block per item; longer ones: shared items
+def test_captured_and_replayed_with_new_lengths(spare):
+    setup = Setup([200, 90], 2, 128, 4, 16, torch.bfloat16, seed=13, spare=spare)
     q = setup.queries(1, 8).to(DEV)
     out = torch.empty_like(q)
-    ws = torch.empty(civic.quant_attention_workspace_bytes(setup.cache, 2, 1, 8), dtype=torch.uint8, device=DEV)
+    ws = torch.empty(max(256, civic.quant_attention_workspace_bytes(setup.cache, 13 + spare, 2, 1, 8)), dtype=torch.uint8, device=DEV)
     lens = setup.lens.clone()
     run = lambda: civic.civic_quant_attention(q, setup.cache, 0, setup.table, lens, out=out, workspace=ws)
     run()
@@ -359,8 +363,9 @@ def test_wrong_shapes_devices_and_types_raise():
                dict(lse=torch.empty((1, 1, 4), device=DEV, dtype=torch.float64))):
         with pytest.raises(ValueError):
             call(**kw)
+    long_table = torch.zeros((1, 33), dtype=torch.int32, device=DEV)
     with pytest.raises(civic.CivicError):
-        call(workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+        call(table=long_table, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
     with pytest.raises(civic.CivicError):
         call(q=setup.queries(1, 5).to(DEV))
     with pytest.raises(civic.CivicError):

@@ -128,7 +128,7 @@ def test_descriptions_that_are_refused(lib, kw, status):
     before = lib.civic_launch_count()
     d = desc(**kw)
     assert lib.civic_quant_page_bytes(d) == 0
-    assert lib.civic_quant_attention_workspace_bytes(d, 1, 1, 4) == 0
+    assert lib.civic_quant_attention_workspace_bytes(d, 100, 1, 1, 4) == 0
     for call in (compact, append, read):
         assert call(lib, d=d) == status
     assert attend(lib, d=d) == status
@@ -198,13 +198,13 @@ def test_attention_refuses_on_the_host(lib):
     assert attend(lib, q=K + 8) == ALIGN
     assert attend(lib, lse=IDX + 2) == ALIGN
     assert attend(lib, st=strides(head=132)) == ALIGN
-    assert attend(lib, ws=None) == WORK
-    assert attend(lib, ws_bytes=100) == WORK
-    assert attend(lib, ws=0x40_0000_0010) == ALIGN
+    assert attend(lib, ws=None, pages=100) == WORK
+    assert attend(lib, ws_bytes=100, pages=100) == WORK
+    assert attend(lib, ws=0x40_0000_0010, pages=100) == ALIGN
     assert attend(lib, out=K) == ARG  # over q
     assert attend(lib, out=C + 16) == ARG  # inside the cache
     assert attend(lib, lse=V) == ARG  # over out
-    assert attend(lib, ws=V - 4096) == ARG
+    assert attend(lib, ws=V - 4096, pages=100) == ARG
     assert attend(lib, n_seq=70000) == UNSUP
     assert attend(lib, q_len=1 << 24) == UNSUP
     assert attend(lib, pages=1 << 28) == UNSUP
