@@ -344,7 +344,7 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     if (st != CIVIC_OK) return st;
     if (max_pages_per_seq < 0 || !std::isfinite(scale)) return CIVIC_ERR_INVALID_ARG;
     const civic_quant_desc_t& d = *desc;
-    if ((int64_t)max_pages_per_seq * d.page_size > INT32_MAX - 64) return CIVIC_ERR_UNSUPPORTED;
+    if ((int64_t)max_pages_per_seq * d.page_size > (1 << 30)) return CIVIC_ERR_UNSUPPORTED;
     if (n_seq == 0 || q_len == 0) return CIVIC_OK;
     if (!q || !cache || !lens || !out || (!block_table && max_pages_per_seq > 0)) return CIVIC_ERR_INVALID_ARG;
     if (!aligned(q, 16) || !aligned(cache, 16) || !aligned(out, 16) || !aligned(block_table, 4) || !aligned(lens, 4) ||
@@ -389,6 +389,8 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     p.group = q_heads / d.n_heads;
     p.causal = causal != 0;
     p.page_tiles = d.page_size / civic::kQuantTile;
+    // exact for tiles below 2^26: tile * (magic * page_tiles - 2^32) < 2^26 * 64 = 2^32
+    p.page_magic = p.page_tiles == 1 ? 0u : (uint32_t)(((1ull << 32) + p.page_tiles - 1) / p.page_tiles);
     p.max_pages = max_pages_per_seq;
     p.n_pages = d.n_pages;
     p.capacity = max_pages_per_seq * d.page_size;

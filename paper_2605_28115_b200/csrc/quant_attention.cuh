@@ -17,7 +17,7 @@
 //
 // fp16 operands, 32-bit accumulators and statistics.  q is scaled by a power of two per row, so that
 // its largest element is in [2^14, 2^15): elements down to 2^-28 of it are still represented.  P' is
-// rounded to fp16 (11 bits): its reference exponent m bounds S + log2(s), not S alone, so that the
+// rounded to fp16 (11 bits; where results are fp16 the remainder goes through a second time): its reference exponent m bounds S + log2(s), not S alone, so that the
 // largest product p s, not the largest p, is near 1.  The reference is lazy: it moves only when some
 // S + log2(s) exceeds it by more than 8 (a warp vote), and then O, l and the minima's sums follow.
 //
@@ -29,6 +29,8 @@
 // joins them in a fixed order.  Where the block tables are short (kQaWholeTiles) a block takes an item as
 // a whole instead: one launch, no workspace.
 #pragma once
+#include <type_traits>
+
 #include "quant_cache.cuh"
 
 namespace civic {
@@ -54,7 +56,8 @@ struct QuantAttnParams {
     int32_t n_seq, q_len, q_heads, n_heads, group;
     int32_t causal;
     int32_t page_tiles, max_pages, n_pages;
-    int32_t capacity;            // tokens the block table can address
+    uint32_t page_magic;         // ceil(2^32 / page_tiles), 0 for 1: tile / page_tiles by one multiplication
+    int32_t capacity;            // tokens the block table can address, at most 2^30
     int32_t blocks;              // of the main kernel where items are shared between blocks; 0 = a block per item
     float scale_log2e;
     int32_t* check;
@@ -170,6 +173,17 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same on T's own type: products of minima (T, exact) with the parts of a sum of q.
+template <typename T>
+__device__ __forceinline__ void mma_minima(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same<T, __half>::value)
+        mma_16x8x16(d, a0, a1, a0, a1, b0, b1);
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %4, %5}, {%6, %7}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
 {
     uint32_t d;
@@ -203,10 +217,14 @@ struct QaWarp {
     static constexpr int NG = Tile::kGroups, MT = HD / 16;
 
     uint32_t q[NT][NG][2][2];  // operand of the first product: [group][depth step][register]
-    float q_sum[NT][2][NG];    // sum over the group of the scaled q, times 2^-24; columns 2 t, 2 t + 1
+    uint32_t q_sum[NT][(NG + 3) / 4][2];  // operand that meets the minima: the sum over group t (+ 4) of q in three parts
     float factor[NT][2];       // takes a raw score to base-2 logits
     int limit[NT][2];          // tokens the column's query row sees
     float ref[NT][2], l[NT][2], v_min[NT][2][NG];
+    bool fresh;                // no tile yet
+    static constexpr bool kHalf = std::is_same<T, __half>::value;
+    // unit of the minima's products: sums of q reach 2^20, and an fp16 must hold them
+    static constexpr float kSumUnit = kHalf ? 0x1p-8f : 0x1p-24f, kMinUnit = kHalf ? 0x1p-16f : 1.f;
     float o[NT][MT][4];
 
     // The item's query rows; only issues the loads.
@@ -232,6 +250,7 @@ struct QaWarp {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         const int head = c.item / c.q.row_blocks, row0 = (c.item - head * c.q.row_blocks) * (8 * NT);
         const int rows = c.q.q_len * p.group;
+        fresh = true;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int row = row0 + nt * 8 + g, token = row / p.group;
@@ -263,7 +282,7 @@ struct QaWarp {
                 }
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-                sums[j] = sum * 0x1p-24f;
+                sums[j] = sum * kSumUnit;
                 if constexpr (BITS == 4) {
                     // nibbles i and i + 4 of a word meet in one operand register; odd ones arrive times 16
                     q[nt][j][0][0] = pack_half2(f[j][0], f[j][4]);
@@ -278,6 +297,18 @@ struct QaWarp {
                     }
                 }
             }
+            // Depths 2 t, 2 t + 1 and 2 t + 8 of that operand are the sum's leading bits, the next ones and the
+            // rest, so that its 16-bit parts add up to fp32's precision; all meet the minimum of group t.
+#pragma unroll
+            for (int pl = 0; pl < (NG + 3) / 4; ++pl) {
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 4 * pl; j < NG && j < 4 * pl + 4; ++j)
+                    if (t == j - 4 * pl) sum = sums[j];
+                const float hi = H::lo(H::pack(sum, 0.f)), mid = H::lo(H::pack(sum - hi, 0.f));
+                q_sum[nt][pl][0] = H::pack(hi, mid);
+                q_sum[nt][pl][1] = H::pack(sum - hi - mid, 0.f);
+            }
             // what belongs to a column of the score tile: from the lanes that hold its query row
             const float fac = down * 0x1p24f * p.scale_log2e;
             const int seen = row < rows ? (p.causal ? min(max(c.q.len - c.q.q_len + token + 1, 0), c.q.len) : c.q.len) : 0;
@@ -286,13 +317,10 @@ struct QaWarp {
                 const int from = (2 * t + b) * 4;
                 factor[nt][b] = __shfl_sync(0xFFFFFFFFu, fac, from);
                 limit[nt][b] = __shfl_sync(0xFFFFFFFFu, seen, from);
-                ref[nt][b] = kQaNoMax;
+                ref[nt][b] = 0.f;
                 l[nt][b] = 0.f;
 #pragma unroll
-                for (int j = 0; j < NG; ++j) {
-                    q_sum[nt][b][j] = __shfl_sync(0xFFFFFFFFu, sums[j], from);
-                    v_min[nt][b][j] = 0.f;
-                }
+                for (int j = 0; j < NG; ++j) v_min[nt][b][j] = 0.f;
             }
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
@@ -333,6 +361,18 @@ struct QaWarp {
         // ---- scores: c[nt] = rows g and g + 8 (tokens), columns 2 t and 2 t + 1 (query rows)
         float c[NT][4] = {};
         {
+#pragma unroll
+            for (int pl = 0; pl < (NG + 3) / 4; ++pl) {
+                const int group = 4 * pl + (NG < 4 ? (t & (NG - 1)) : t);  // lanes without a group meet zeros
+                const uint32_t a0 = __byte_perm(kp[g * NG + group], 0, 0x3232), a1 = __byte_perm(kp[(g + 8) * NG + group], 0, 0x3232);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_minima<T>(c[nt], a0, a1, q_sum[nt][pl][0], q_sum[nt][pl][1]);
+            }
+            if constexpr (kHalf)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) c[nt][i] *= kMinUnit;
             uint32_t par[2][NG];
             load(par[0], kp + g * NG);
             load(par[1], kp + (g + 8) * NG);
@@ -374,7 +414,7 @@ struct QaWarp {
                         for (int r = 0; r < 2; ++r)
 #pragma unroll
                             for (int b = 0; b < 2; ++b)
-                                c[nt][2 * r + b] += H::lo(par[r][j]) * d[2 * r + b] + H::hi(par[r][j]) * q_sum[nt][b][j];
+                                c[nt][2 * r + b] = fmaf(H::lo(par[r][j]), d[2 * r + b], c[nt][2 * r + b]);
                     }
                 }
             }
@@ -383,38 +423,50 @@ struct QaWarp {
         uint32_t par[2][NG];
         load(par[0], vp + g * NG);
         load(par[1], vp + (g + 8) * NG);
-        float lift[2];  // about log2 of the token's largest V scale
+        float lift[2];  // log2 of a power of two at or above the token's largest V scale
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            float s = H::lo(par[r][0]);
+            if constexpr (kHalf) {
+                float s = H::lo(par[r][0]);
 #pragma unroll
-            for (int j = 1; j < NG; ++j) s = fmaxf(s, H::lo(par[r][j]));
-            lift[r] = (float)min(max((int)(__float_as_uint(s) >> 23) - 126, -90), 90);
+                for (int j = 1; j < NG; ++j) s = fmaxf(s, H::lo(par[r][j]));
+                lift[r] = fminf((float)((int)(__float_as_uint(s) >> 23) - 126), 100.f);
+            } else {
+                uint32_t s = par[r][0];  // bf16 scales are not negative: their bit patterns compare like the numbers
+#pragma unroll
+                for (int j = 1; j < NG; ++j) s = __vmaxu2(s, par[r][j]);
+                // between 2^-90 and 2^100 (a NaN's exponent too), so that weights times 2^-lift neither overflow nor
+                // vanish; made a float by the bits of 2^23 + exponent
+                lift[r] = __uint_as_float(min(max((s >> 7) & 0x1FFu, 36u), 226u) | 0x4B000000u) - (8388608.f + 126.f);
+            }
         }
         bool move = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    float& s = c[nt][2 * r + b];
-                    s *= factor[nt][b];
+                    float& s = c[nt][2 * r + b];  // from here on relative to the reference
+                    s = fmaf(s, factor[nt][b], -ref[nt][b]);
                     if (MASK && pos + g + 8 * r >= limit[nt][b]) s = -INFINITY;
-                    move |= s + lift[r] > ref[nt][b] + kQaSlack;
+                    move |= s + lift[r] > kQaSlack;
                 }
-            }
-        if (__any_sync(0xFFFFFFFFu, move)) {
+        if (__any_sync(0xFFFFFFFFu, move) || fresh) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    float top = fmaxf(c[nt][b] + lift[0], c[nt][2 + b] + lift[1]);
+                    float up = fmaxf(c[nt][b] + lift[0], c[nt][2 + b] + lift[1]);
 #pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-                    top = fmaxf(top, ref[nt][b]);
-                    const float f = exp2_fast(ref[nt][b] - top);
-                    ref[nt][b] = top;
+                    for (int d = 4; d < 32; d <<= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, d));
+                    // the first tile sets the reference; a column that sees nothing in it sees nothing at all (tiles come
+                    // in ascending order)
+                    up = fresh && up > -INFINITY ? up : fmaxf(up, 0.f);
+                    const float f = fresh ? 0.f : exp2_fast(-up);
+                    ref[nt][b] += up;
+                    c[nt][b] -= up;
+                    c[nt][2 + b] -= up;
                     l[nt][b] *= f;
 #pragma unroll
                     for (int j = 0; j < NG; ++j) v_min[nt][b][j] *= f;
@@ -424,6 +476,7 @@ struct QaWarp {
                         o[nt][mt][2 + b] *= f;
                     }
                 }
+            fresh = false;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -432,7 +485,7 @@ struct QaWarp {
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     float& x = c[nt][2 * r + b];
-                    x = exp2_fast(x - ref[nt][b]);
+                    x = exp2_fast(x);
                     l[nt][b] += x;
                 }
         // ---- O^T += V^T P'^T, group by group
@@ -475,15 +528,24 @@ struct QaWarp {
                             x[2 * r + b] = scaled;
                             v_min[nt][b][j] += low;
                         }
-                    const uint32_t b0 = transpose_8x8(pack_half2(x[0], x[1])), b1 = transpose_8x8(pack_half2(x[2], x[3]));
+                    const uint32_t p01 = pack_half2(x[0], x[1]), p23 = pack_half2(x[2], x[3]);
+                    const uint32_t b0 = transpose_8x8(p01), b1 = transpose_8x8(p23);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) mma_16x8x16(o[nt][2 * j + h], a[h][0], a[h][1], a[h][2], a[h][3], b0, b1);
+                    if constexpr (kHalf) {
+                        // an fp16 result has as many bits as P' here: what the rounding left goes through as well
+                        using F = Half16<__half>;
+                        const uint32_t r0 = transpose_8x8(pack_half2(x[0] - F::lo(p01), x[1] - F::hi(p01)));
+                        const uint32_t r1 = transpose_8x8(pack_half2(x[2] - F::lo(p23), x[3] - F::hi(p23)));
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) mma_16x8x16(o[nt][2 * j + h], a[h][0], a[h][1], a[h][2], a[h][3], r0, r1);
+                    }
                 }
             }
         }
     }
 
-    // Sums over the lanes that share a column; then every lane of a column's quad has them.
+    // Sums over the lanes that share a column; a column without a token has no reference.
     __device__ __forceinline__ void finish()
     {
 #pragma unroll
@@ -496,6 +558,11 @@ struct QaWarp {
 #pragma unroll
                     for (int j = 0; j < NG; ++j) v_min[nt][b][j] += __shfl_xor_sync(0xFFFFFFFFu, v_min[nt][b][j], d);
                 }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                if (l[nt][b] == 0.f) ref[nt][b] = kQaNoMax;
     }
     // Channels 32 j + 4 g .. + 3 of column b.
     __device__ __forceinline__ float4 output(int nt, int b, int j) const
@@ -583,27 +650,39 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
         if (begin + warp < end) page = page_of(ahead);
         w.load_q(p, cur, x);
     }
-    // the producer side of this warp: tiles begin + warp, + kQaWarps, ...
-    long long next = begin + warp;
+    // the producer side of this warp: `left` tiles, begin + warp, + kQaWarps, ...
+    int left = begin + warp < end ? (int)((end - begin - warp + kQaWarps - 1) / kQaWarps) : 0;
     uint32_t valid = 0;  // bit per stage: the tile was found
+    const int64_t page_stride = (int64_t)p.n_heads * p.page_tiles * Tile::kBytes;
+    const char* base = nullptr;         // the item's K/V head within a page, this lane's first 16 bytes
+    const int32_t* table_row = nullptr;
+    auto enter = [&]() {
+        base = p.cache + (int64_t)(ahead.item / ahead.q.row_blocks) * p.page_tiles * Tile::kBytes + lane * 16;
+        table_row = p.block_table + (size_t)ahead.seq * table_pages;
+    };
+    auto page_slot = [&](int tile) { return p.page_magic ? (int)__umulhi((uint32_t)tile, p.page_magic) : tile; };
+    if (left > 0) enter();
     auto fetch = [&](int stage) {
         valid &= ~(1u << stage);
-        if (next < end) {
+        if (left > 0) {
+            const int slot = page_slot(ahead.tile);
             if ((uint32_t)page < (uint32_t)p.n_pages) {
-                const int head = ahead.item / ahead.q.row_blocks;
-                const char* src = p.cache + (((size_t)page * p.n_heads + head) * p.page_tiles + ahead.tile % p.page_tiles) * Tile::kBytes;
-                uint8_t* dst = ring + stage * Tile::kBytes;
+                const char* src = base + page * page_stride + (ahead.tile - slot * p.page_tiles) * Tile::kBytes;
+                uint8_t* dst = ring + stage * Tile::kBytes + lane * 16;
 #pragma unroll
-                for (int i = 0; i < Tile::kBytes / 16; i += 32)
-                    if (i + lane < Tile::kBytes / 16) cp_async16(dst + (i + lane) * 16, src + (i + lane) * 16);
+                for (int i = 0; i < Tile::kBytes; i += 512)
+                    if (i + 512 <= Tile::kBytes || i + lane * 16 < Tile::kBytes) cp_async16(dst + i, src + i);
                 valid |= 1u << stage;
             } else if (p.check && lane == 0) {
-                report_bad_index(p.check, kIndexBadPage, ahead.seq, ahead.tile / p.page_tiles, page);
+                report_bad_index(p.check, kIndexBadPage, ahead.seq, slot, page);
             }
-            next += kQaWarps;
-            if (next < end) {
-                qa_advance<kRows>(p, ahead, kQaWarps);
-                page = page_of(ahead);  // used one tile later
+            if (--left > 0) {
+                ahead.tile += kQaWarps;
+                if (ahead.tile >= ahead.q.tiles) {
+                    qa_advance<kRows>(p, ahead, 0);
+                    enter();
+                }
+                page = __ldg(table_row + page_slot(ahead.tile));  // used one tile later
             }
         }
         cp_async_commit();
@@ -611,8 +690,8 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
 #pragma unroll
     for (int st = 0; st < kStages; ++st) fetch(st);
 
-    long long at = begin, mine = begin + warp;
-    int stage = 0;
+    long long at = begin;
+    int stage = 0, skip = warp;  // tiles of the segment before this warp's first
     do {
         // one item's tiles inside this block's share: [at, to)
         const long long item_end = at + (cur.q.tiles - cur.tile), to = min(end, item_end);
@@ -622,11 +701,13 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
         for (int nt = 0; nt < NT; ++nt) sees_all = min(sees_all, min(w.limit[nt][0], w.limit[nt][1]));
 #pragma unroll
         for (int d = 1; d < 4; d <<= 1) sees_all = min(sees_all, __shfl_xor_sync(0xFFFFFFFFu, sees_all, d));
-        for (; mine < to; mine += kQaWarps) {
+        const int taken = (int)(to - at);
+        int mine = skip;
+        for (; mine < taken; mine += kQaWarps) {
             cp_async_wait<kStages - 1>();
             __syncwarp();
             if ((valid >> stage) & 1) {
-                const int pos = (cur.tile + (int)(mine - at)) * kQuantTile;
+                const int pos = (cur.tile + mine) * kQuantTile;
                 const uint8_t* tile = ring + stage * Tile::kBytes;
                 if (pos + kQuantTile <= sees_all) w.template step<false>(tile, pos);
                 else w.template step<true>(tile, pos);
@@ -684,7 +765,7 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
             }
             __syncthreads();
         }
-        const int taken = (int)(to - at);
+        skip = mine - taken;
         at = to;
         if (at < end) {
             qa_advance<kRows>(p, cur, taken);
