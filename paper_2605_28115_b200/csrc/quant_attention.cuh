@@ -197,9 +197,28 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ void cp_async16(void* dst, const void* src)
+template <int OFFSET>
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0 + %2], [%1 + %2], 16;" ::"r"(dst), "l"(src), "n"(OFFSET) : "memory");
+}
+// BYTES from src to dst by a warp; both point at the lane's first 16 bytes
+template <int BYTES, int AT = 0>
+__device__ __forceinline__ void cp_async_tile(uint32_t dst, const char* src, int lane)
+{
+    if constexpr (AT + 512 <= BYTES) {
+        cp_async16<AT>(dst, src);
+        cp_async_tile<BYTES, AT + 512>(dst, src, lane);
+    } else if constexpr (AT < BYTES) {
+        if (AT + lane * 16 < BYTES) cp_async16<AT>(dst, src);
+    }
+}
+// a * b + c, limited to [0, 1]
+__device__ __forceinline__ float fma_sat(float a, float b, float c)
+{
+    float d;
+    asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -311,7 +330,8 @@ struct QaWarp {
             }
             // what belongs to a column of the score tile: from the lanes that hold its query row
             const float fac = down * 0x1p24f * p.scale_log2e;
-            const int seen = row < rows ? (p.causal ? min(max(c.q.len - c.q.q_len + token + 1, 0), c.q.len) : c.q.len) : 0;
+            // columns behind the last row are computed and not stored: they must not make tiles need a mask
+            const int seen = p.causal && row < rows ? min(max(c.q.len - c.q.q_len + token + 1, 0), c.q.len) : c.q.len;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const int from = (2 * t + b) * 4;
@@ -423,21 +443,24 @@ struct QaWarp {
         uint32_t par[2][NG];
         load(par[0], vp + g * NG);
         load(par[1], vp + (g + 8) * NG);
-        float lift[2];  // log2 of a power of two at or above the token's largest V scale
+        // About log2 of the token's largest V scale (at most 0.09 below, by the number's bits: exponent and
+        // mantissa read as one fixed-point number), limited to -90 .. 100 so that weights times 2^-lift neither
+        // overflow nor vanish: lift = 190 y - 90
+        float y[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             if constexpr (kHalf) {
                 float s = H::lo(par[r][0]);
 #pragma unroll
                 for (int j = 1; j < NG; ++j) s = fmaxf(s, H::lo(par[r][j]));
-                lift[r] = fminf((float)((int)(__float_as_uint(s) >> 23) - 126), 100.f);
+                // as above from the fp32 pattern, of which 16 bits are enough
+                y[r] = fma_sat(__uint_as_float(__byte_perm(__float_as_uint(s), 0x4B00u, 0x5432)), 1.f / (128 * 190),
+                               -(65536.f + 127.f - 90.f) / 190);
             } else {
                 uint32_t s = par[r][0];  // bf16 scales are not negative: their bit patterns compare like the numbers
 #pragma unroll
                 for (int j = 1; j < NG; ++j) s = __vmaxu2(s, par[r][j]);
-                // between 2^-90 and 2^100 (a NaN's exponent too), so that weights times 2^-lift neither overflow nor
-                // vanish; made a float by the bits of 2^23 + exponent
-                lift[r] = __uint_as_float(min(max((s >> 7) & 0x1FFu, 36u), 226u) | 0x4B000000u) - (8388608.f + 126.f);
+                y[r] = fma_sat(__uint_as_float(__byte_perm(s, 0x4B00u, 0x5410)), 1.f / (128 * 190), -(65536.f + 127.f - 90.f) / 190);
             }
         }
         bool move = false;
@@ -450,14 +473,14 @@ struct QaWarp {
                     float& s = c[nt][2 * r + b];  // from here on relative to the reference
                     s = fmaf(s, factor[nt][b], -ref[nt][b]);
                     if (MASK && pos + g + 8 * r >= limit[nt][b]) s = -INFINITY;
-                    move |= s + lift[r] > kQaSlack;
+                    move |= fmaf(y[r], 190.f, s) > kQaSlack + 90.f;
                 }
         if (__any_sync(0xFFFFFFFFu, move) || fresh) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    float up = fmaxf(c[nt][b] + lift[0], c[nt][2 + b] + lift[1]);
+                    float up = fmaxf(fmaf(y[0], 190.f, c[nt][b]), fmaf(y[1], 190.f, c[nt][2 + b])) - 90.f;
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) up = fmaxf(up, __shfl_xor_sync(0xFFFFFFFFu, up, d));
                     // the first tile sets the reference; a column that sees nothing in it sees nothing at all (tiles come
@@ -600,8 +623,15 @@ __device__ __forceinline__ void qa_store(const QuantAttnParams& p, int seq, int 
     if (channel == 0 && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
+// Blocks per SM that the register budget is set for.
+template <int HD, int NT>
+__host__ __device__ constexpr int qa_min_blocks()
+{
+    return HD * NT <= 64 ? 4 : (HD * NT <= 128 ? 3 : 2);
+}
+
 template <typename T, int HD, int BITS, int NT>
-__global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __grid_constant__ QuantAttnParams p)
+__global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_attention_kernel(const __grid_constant__ QuantAttnParams p)
 {
     using Tile = QuantTile<HD, BITS>;
     constexpr int kStages = qa_stages<HD, BITS>(), kRows = 8 * NT;
@@ -652,7 +682,8 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
     }
     // the producer side of this warp: `left` tiles, begin + warp, + kQaWarps, ...
     int left = begin + warp < end ? (int)((end - begin - warp + kQaWarps - 1) / kQaWarps) : 0;
-    uint32_t valid = 0;  // bit per stage: the tile was found
+    uint32_t lost = 0;  // bit per stage: its tile's page is none
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
     const int64_t page_stride = (int64_t)p.n_heads * p.page_tiles * Tile::kBytes;
     const char* base = nullptr;         // the item's K/V head within a page, this lane's first 16 bytes
     const int32_t* table_row = nullptr;
@@ -663,18 +694,15 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
     auto page_slot = [&](int tile) { return p.page_magic ? (int)__umulhi((uint32_t)tile, p.page_magic) : tile; };
     if (left > 0) enter();
     auto fetch = [&](int stage) {
-        valid &= ~(1u << stage);
+        lost &= ~(1u << stage);
         if (left > 0) {
             const int slot = page_slot(ahead.tile);
             if ((uint32_t)page < (uint32_t)p.n_pages) {
                 const char* src = base + page * page_stride + (ahead.tile - slot * p.page_tiles) * Tile::kBytes;
-                uint8_t* dst = ring + stage * Tile::kBytes + lane * 16;
-#pragma unroll
-                for (int i = 0; i < Tile::kBytes; i += 512)
-                    if (i + 512 <= Tile::kBytes || i + lane * 16 < Tile::kBytes) cp_async16(dst + i, src + i);
-                valid |= 1u << stage;
-            } else if (p.check && lane == 0) {
-                report_bad_index(p.check, kIndexBadPage, ahead.seq, slot, page);
+                cp_async_tile<Tile::kBytes>(ring_at + stage * Tile::kBytes, src, lane);
+            } else {
+                lost |= 1u << stage;
+                if (p.check && lane == 0) report_bad_index(p.check, kIndexBadPage, ahead.seq, slot, page);
             }
             if (--left > 0) {
                 ahead.tile += kQaWarps;
@@ -706,7 +734,7 @@ __global__ void __launch_bounds__(kQaThreads) quant_attention_kernel(const __gri
         for (; mine < taken; mine += kQaWarps) {
             cp_async_wait<kStages - 1>();
             __syncwarp();
-            if ((valid >> stage) & 1) {
+            if (!((lost >> stage) & 1)) {
                 const int pos = (cur.tile + mine) * kQuantTile;
                 const uint8_t* tile = ring + stage * Tile::kBytes;
                 if (pos + kQuantTile <= sees_all) w.template step<false>(tile, pos);
