@@ -400,6 +400,8 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     const int64_t rows = (int64_t)q_len * p.group;
     const int nt = attention_tiles(d.head_dim, rows);
     const unsigned items = (unsigned)((rows + 8 * nt - 1) / (8 * nt) * d.n_heads);
+    // a block's share of the tiles, of at least 148 blocks', is counted in 32 bits
+    if ((double)n_seq * items * (p.capacity / civic::kQuantTile) > 148.0 * (1 << 30)) return CIVIC_ERR_UNSUPPORTED;
     return d.dtype == CIVIC_BF16 ? launch_attention_dim<__nv_bfloat16>(d, nt, p, items, (cudaStream_t)stream)
                                  : launch_attention_dim<__half>(d, nt, p, items, (cudaStream_t)stream);
 }

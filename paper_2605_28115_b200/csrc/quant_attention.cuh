@@ -117,6 +117,19 @@ __host__ __device__ inline long long qa_share(long long total, int blocks)
     return even < kQaMinTiles ? kQaMinTiles : even;
 }
 
+// The same value in all lanes, in a form that the compiler sees: branches on it need no convergence code.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+template <int ROWS>
+__device__ __forceinline__ QaSeq qa_sequence_uniform(const QuantAttnParams& p, int s)
+{
+    QaSeq q = qa_sequence<ROWS>(p, s);
+    q.len = uniform(q.len);
+    q.q_len = uniform(q.q_len);
+    q.tiles = uniform(q.tiles);
+    q.row_blocks = uniform(q.row_blocks);
+    return q;
+}
+
 // A place in the line of units.
 struct QaCursor {
     int seq, item, tile;  // item = head * row_blocks + row block
@@ -138,10 +151,10 @@ __device__ __forceinline__ QaCursor qa_locate(const QuantAttnParams& p, long lon
         if (past) {
             const int l = __ffs(past) - 1;
             const long long rest = unit - __shfl_sync(0xFFFFFFFFu, upto - u, l);
-            c.seq = s0 + l;
-            c.q = qa_sequence<ROWS>(p, c.seq);
-            c.item = (int)(rest / c.q.tiles);
-            c.tile = (int)(rest - (long long)c.item * c.q.tiles);
+            c.seq = uniform(s0 + l);
+            c.q = qa_sequence_uniform<ROWS>(p, c.seq);
+            c.item = uniform((int)(rest / c.q.tiles));
+            c.tile = uniform((int)(rest - (long long)c.item * c.q.tiles));
             return c;
         }
         before = __shfl_sync(0xFFFFFFFFu, upto, 31);
@@ -159,8 +172,8 @@ __device__ __forceinline__ void qa_advance(const QuantAttnParams& p, QaCursor& c
         c.item = 0;
         do {
             if (++c.seq >= p.n_seq) return;
-            c.q = qa_sequence<ROWS>(p, c.seq);
-        } while (c.q.units == 0);
+            c.q = qa_sequence_uniform<ROWS>(p, c.seq);
+        } while (c.q.tiles == 0 || c.q.row_blocks == 0);
     }
 }
 
@@ -646,7 +659,7 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
     QaWarp<T, HD, BITS, NT> w;
     uint4 x[NT][Tile::kGroups];
     QaCursor cur, ahead;
-    long long begin, end;
+    int units;       // this block's share
     int page = -1;  // of this warp's next tile
     const int table_pages = p.max_pages;
     auto page_of = [&](const QaCursor& c) {
@@ -661,27 +674,26 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
         cur.q.row_blocks = (p.q_len * p.group + kRows - 1) / kRows;  // with q_lens: as many blocks per head as the longest needs
         w.load_q(p, cur, x);
         const int row_blocks = cur.q.row_blocks;
-        cur.q = qa_sequence<kRows>(p, cur.seq);
+        cur.q = qa_sequence_uniform<kRows>(p, cur.seq);
         if (cur.item % row_blocks >= cur.q.row_blocks) return;
         cur.q.row_blocks = row_blocks;
         ahead = cur;
         ahead.tile = warp;
-        begin = 0;
-        end = cur.q.tiles;
+        units = cur.q.tiles;
     } else {
         long long unused;
         const long long total = qa_total<kRows>(p, 0, unused), share = qa_share(total, p.blocks);
-        begin = blockIdx.x * share;
-        end = min(begin + share, total);
+        const long long begin = blockIdx.x * share, end = min(begin + share, total);
         if (begin >= end) return;
+        units = uniform((int)(end - begin));  // fewer than 2^31 by the host's check
         cur = qa_locate<kRows>(p, begin);
         ahead = cur;
         qa_advance<kRows>(p, ahead, warp);
-        if (begin + warp < end) page = page_of(ahead);
+        if (warp < units) page = page_of(ahead);
         w.load_q(p, cur, x);
     }
-    // the producer side of this warp: `left` tiles, begin + warp, + kQaWarps, ...
-    int left = begin + warp < end ? (int)((end - begin - warp + kQaWarps - 1) / kQaWarps) : 0;
+    // the producer side of this warp: `left` tiles, numbers warp, warp + kQaWarps, ... of the share
+    int left = (units - warp + kQaWarps - 1) / kQaWarps;
     uint32_t lost = 0;  // bit per stage: its tile's page is none
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
     const int64_t page_stride = (int64_t)p.n_heads * p.page_tiles * Tile::kBytes;
@@ -697,7 +709,7 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
         lost &= ~(1u << stage);
         if (left > 0) {
             const int slot = page_slot(ahead.tile);
-            if ((uint32_t)page < (uint32_t)p.n_pages) {
+            if (__all_sync(0xFFFFFFFFu, (uint32_t)page < (uint32_t)p.n_pages)) {
                 const char* src = base + page * page_stride + (ahead.tile - slot * p.page_tiles) * Tile::kBytes;
                 cp_async_tile<Tile::kBytes>(ring_at + stage * Tile::kBytes, src, lane);
             } else {
@@ -718,18 +730,18 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
 #pragma unroll
     for (int st = 0; st < kStages; ++st) fetch(st);
 
-    long long at = begin;
+    int at = 0;
     int stage = 0, skip = warp;  // tiles of the segment before this warp's first
     do {
-        // one item's tiles inside this block's share: [at, to)
-        const long long item_end = at + (cur.q.tiles - cur.tile), to = min(end, item_end);
+        // one item's tiles inside this block's share
+        const int taken = min(units - at, cur.q.tiles - cur.tile);
         w.begin(p, cur, x);
         int sees_all = w.limit[0][0];  // tokens that every column of the warp sees
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sees_all = min(sees_all, min(w.limit[nt][0], w.limit[nt][1]));
 #pragma unroll
         for (int d = 1; d < 4; d <<= 1) sees_all = min(sees_all, __shfl_xor_sync(0xFFFFFFFFu, sees_all, d));
-        const int taken = (int)(to - at);
+        sees_all = uniform(sees_all);
         int mine = skip;
         for (; mine < taken; mine += kQaWarps) {
             cp_async_wait<kStages - 1>();
@@ -749,7 +761,7 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
         const int g = lane >> 2, t = lane & 3;
         const int head = cur.item / cur.q.row_blocks, row0 = (cur.item - head * cur.q.row_blocks) * kRows;
         const int rows = min(kRows, cur.q.q_len * p.group - row0);
-        const bool whole = cur.tile == 0 && to == item_end;
+        const bool whole = cur.tile == 0 && taken == cur.q.tiles;
         float* slot = p.partial + (size_t)(2 * blockIdx.x + (cur.tile > 0 ? 0 : 1)) * kRows * (HD + 2);
         if (g == 0)
 #pragma unroll
@@ -794,12 +806,12 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
             __syncthreads();
         }
         skip = mine - taken;
-        at = to;
-        if (at < end) {
+        at += taken;
+        if (at < units) {
             qa_advance<kRows>(p, cur, taken);
             w.load_q(p, cur, x);
         }
-    } while (at < end);
+    } while (at < units);
 }
 
 // Joins the partial results of items that several blocks shared; writes the rows of sequences without
