@@ -570,7 +570,7 @@ civic_status_t civic_read_kv_quant(const void* const* cache, const civic_quant_d
  * Weights and codes are multiplied as fp16 with fp32 accumulation, scores, sums and lse are fp32.  V
  * groups' scales are expected within 2^-86 .. 2^100, scores may have any size; max_pages_per_seq *
  * page_size <= 2^30 (CIVIC_ERR_UNSUPPORTED).  One launch where
- * max_pages_per_seq * page_size <= 512, two otherwise.
+ * max_pages_per_seq * page_size <= 1024, two otherwise.
  */
 civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q_strides, const void* cache,
                                      const civic_quant_desc_t* desc, const int32_t* block_table, int32_t max_pages_per_seq,

@@ -214,28 +214,34 @@ int attention_tiles(int head_dim, int64_t rows)
 template <typename T, int HD, int BITS, int NT>
 civic_status_t launch_attention(civic::QuantAttnParams& p, unsigned items, cudaStream_t stream)
 {
-    const auto kernel = civic::quant_attention_kernel<T, HD, BITS, NT>;
-    constexpr size_t smem = civic::qa_smem_bytes<HD, BITS, NT>();
-    static_assert(smem <= kMaxDynamicSmem, "the ring and the join area fit into shared memory");
-    static std::atomic<int> allowed[64], resident[64];
-    const civic_status_t as = allow_dynamic_smem(kernel, smem, allowed);
+    const bool pdl = programmatic();
+    static std::atomic<int> allowed[2][64], resident[64];
+    if (p.blocks == 0) {
+        constexpr int kWarps = civic::kQaWholeWarps;
+        const auto kernel = civic::quant_attention_kernel<T, HD, BITS, NT, kWarps>;
+        constexpr size_t smem = civic::qa_smem_bytes<HD, BITS, NT, kWarps>();
+        static_assert(smem <= kMaxDynamicSmem, "the rings and the join area fit into shared memory");
+        const civic_status_t as = allow_dynamic_smem(kernel, smem, allowed[0]);
+        if (as != CIVIC_OK) return as;
+        CIVIC_CUDA_TRY(civic::launch(pdl, kernel, dim3(items, (unsigned)p.n_seq), 32u * kWarps, smem, stream, p));
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+        return CIVIC_OK;
+    }
+    constexpr int kWarps = civic::kQaWarps;
+    const auto kernel = civic::quant_attention_kernel<T, HD, BITS, NT, kWarps>;
+    constexpr size_t smem = civic::qa_smem_bytes<HD, BITS, NT, kWarps>();
+    const civic_status_t as = allow_dynamic_smem(kernel, smem, allowed[1]);
     if (as != CIVIC_OK) return as;
     const int dev = device_slot();
     int per_sm = dev >= 0 ? resident[dev].load(std::memory_order_relaxed) : 0;
     if (per_sm == 0) {
-        CIVIC_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, civic::kQaThreads, smem));
+        CIVIC_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, 32 * kWarps, smem));
         if (per_sm < 1) return CIVIC_ERR_UNSUPPORTED;
         if (dev >= 0) resident[dev].store(per_sm, std::memory_order_relaxed);
     }
-    const bool pdl = programmatic();
-    if (p.blocks == 0) {
-        CIVIC_CUDA_TRY(civic::launch(pdl, kernel, dim3(items, (unsigned)p.n_seq), (unsigned)civic::kQaThreads, smem, stream, p));
-        g_launches.fetch_add(1, std::memory_order_relaxed);
-        return CIVIC_OK;
-    }
     const int blocks = sm_count() * per_sm;
     p.blocks = blocks < civic::kQaMaxBlocks ? blocks : civic::kQaMaxBlocks;
-    CIVIC_CUDA_TRY(civic::launch(pdl, kernel, (unsigned)p.blocks, (unsigned)civic::kQaThreads, smem, stream, p));
+    CIVIC_CUDA_TRY(civic::launch(pdl, kernel, (unsigned)p.blocks, 32u * kWarps, smem, stream, p));
     CIVIC_CUDA_TRY(civic::launch(pdl, civic::quant_attention_join_kernel<T, HD, NT>, dim3(items, (unsigned)p.n_seq),
                                  (unsigned)(HD / 4 * 8), 0, stream, p));
     g_launches.fetch_add(2, std::memory_order_relaxed);

@@ -35,11 +35,11 @@
 
 namespace civic {
 
-constexpr int kQaWarps = 4;
-constexpr int kQaThreads = 32 * kQaWarps;
+constexpr int kQaWarps = 4;        // warps of a block where items are shared
+constexpr int kQaWholeWarps = 8;   // and where a block takes an item as a whole: 128 items of 26 tiles 8.8 -> 7.0 us
 constexpr int kQaMaxBlocks = 148 * 4;  // also fixes the workspace size
 constexpr int kQaMinTiles = 2 * kQaWarps;
-constexpr int kQaWholeTiles = 32;      // tables up to this many tiles: a block per item, nothing to join
+constexpr int kQaWholeTiles = 64;      // tables up to this many tiles: a block per item, nothing to join
 constexpr float kQaNoMax = -1e30f;     // reference of a row that has seen nothing
 constexpr float kQaSlack = 8.f;        // P' stays below 2^9
 
@@ -617,10 +617,10 @@ __host__ __device__ constexpr int qa_stages()
     return n < 2 ? 2 : (n > 6 ? 6 : n);
 }
 // ring | O of every warp, one n-tile at a time | reference and sum of every warp and row
-template <int HD, int BITS, int NT>
+template <int HD, int BITS, int NT, int W>
 __host__ __device__ constexpr size_t qa_smem_bytes()
 {
-    return (size_t)kQaWarps * (qa_stages<HD, BITS>() * quant_tile_bytes(HD, BITS) + 8 * HD * 4 + NT * 8 * 8);
+    return (size_t)W * (qa_stages<HD, BITS>() * quant_tile_bytes(HD, BITS) + 8 * HD * 4 + NT * 8 * 8);
 }
 
 // out and lse of one row from the sums over its tokens
@@ -643,15 +643,15 @@ __host__ __device__ constexpr int qa_min_blocks()
     return HD * NT <= 64 ? 4 : (HD * NT <= 128 ? 3 : 2);
 }
 
-template <typename T, int HD, int BITS, int NT>
-__global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_attention_kernel(const __grid_constant__ QuantAttnParams p)
+template <typename T, int HD, int BITS, int NT, int W>
+__global__ void __launch_bounds__(32 * W, W == kQaWarps ? qa_min_blocks<HD, NT>() : 1) quant_attention_kernel(const __grid_constant__ QuantAttnParams p)
 {
     using Tile = QuantTile<HD, BITS>;
     constexpr int kStages = qa_stages<HD, BITS>(), kRows = 8 * NT;
     extern __shared__ __align__(16) uint8_t qa_smem[];
     uint8_t* ring_all = qa_smem;
-    float* o_sm = reinterpret_cast<float*>(qa_smem + kQaWarps * kStages * Tile::kBytes);  // [warp][8][HD]
-    float2* ml_sm = reinterpret_cast<float2*>(o_sm + kQaWarps * 8 * HD);                  // [warp][rows]
+    float* o_sm = reinterpret_cast<float*>(qa_smem + W * kStages * Tile::kBytes);  // [warp][8][HD]
+    float2* ml_sm = reinterpret_cast<float2*>(o_sm + W * 8 * HD);                  // [warp][rows]
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     uint8_t* ring = ring_all + warp * kStages * Tile::kBytes;
     release_next_kernel();  // the joining kernel is small: its blocks may wait beside this one's
@@ -692,8 +692,8 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
         if (warp < units) page = page_of(ahead);
         w.load_q(p, cur, x);
     }
-    // the producer side of this warp: `left` tiles, numbers warp, warp + kQaWarps, ... of the share
-    int left = (units - warp + kQaWarps - 1) / kQaWarps;
+    // the producer side of this warp: `left` tiles, numbers warp, warp + W, ... of the share
+    int left = (units - warp + W - 1) / W;
     uint32_t lost = 0;  // bit per stage: its tile's page is none
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
     const int64_t page_stride = (int64_t)p.n_heads * p.page_tiles * Tile::kBytes;
@@ -717,7 +717,7 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
                 if (p.check && lane == 0) report_bad_index(p.check, kIndexBadPage, ahead.seq, slot, page);
             }
             if (--left > 0) {
-                ahead.tile += kQaWarps;
+                ahead.tile += W;
                 if (ahead.tile >= ahead.q.tiles) {
                     qa_advance<kRows>(p, ahead, 0);
                     enter();
@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
         for (int d = 1; d < 4; d <<= 1) sees_all = min(sees_all, __shfl_xor_sync(0xFFFFFFFFu, sees_all, d));
         sees_all = uniform(sees_all);
         int mine = skip;
-        for (; mine < taken; mine += kQaWarps) {
+        for (; mine < taken; mine += W) {
             cp_async_wait<kStages - 1>();
             __syncwarp();
             if (!((lost >> stage) & 1)) {
@@ -776,15 +776,15 @@ __global__ void __launch_bounds__(kQaThreads, qa_min_blocks<HD, NT>()) quant_att
                 for (int j = 0; j < HD / 32; ++j)
                     *reinterpret_cast<float4*>(o_sm + (warp * 8 + 2 * t + b) * HD + j * 32 + g * 4) = w.output(nt, b, j);
             __syncthreads();
-            for (int i = threadIdx.x; i < 8 * HD / 4; i += kQaThreads) {
+            for (int i = threadIdx.x; i < 8 * HD / 4; i += 32 * W) {
                 const int col = i / (HD / 4), ch = (i - col * (HD / 4)) * 4, row = nt * 8 + col;
                 if (row >= rows) continue;
                 float m = kQaNoMax, l = 0.f;
 #pragma unroll
-                for (int k = 0; k < kQaWarps; ++k) m = fmaxf(m, ml_sm[k * kRows + row].x);
+                for (int k = 0; k < W; ++k) m = fmaxf(m, ml_sm[k * kRows + row].x);
                 float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int k = 0; k < kQaWarps; ++k) {
+                for (int k = 0; k < W; ++k) {
                     const float2 ml = ml_sm[k * kRows + row];
                     const float f = exp2_fast(ml.x - m);
                     const float4 x = *reinterpret_cast<const float4*>(o_sm + (k * 8 + col) * HD + ch);

@@ -133,7 +133,7 @@ SHAPES = [  # lens, heads, q_heads, dim, bits, page, q_len, dtype
 
 @pytest.mark.parametrize("case", SHAPES)
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("spare", [0, 33])  # tables beyond 512 tokens take the kernels that share items between blocks
+@pytest.mark.parametrize("spare", [0, 65])  # tables beyond 1024 tokens take the kernels that share items between blocks
 def test_against_64_bits(case, causal, spare):
     lens, heads, q_heads, dim, bits, page, q_len, dtype = case
     setup = Setup(lens, heads, dim, bits, page, dtype, seed=3, spare=spare)
@@ -144,7 +144,7 @@ def test_against_64_bits(case, causal, spare):
     assert torch.equal(out, again) and torch.equal(lse, lse2)
 
 
-@pytest.mark.parametrize("spare", [0, 33])
+@pytest.mark.parametrize("spare", [0, 65])
 def test_padded_queries_and_rows_that_see_nothing(spare):
     setup = Setup([40, 3, 100, 0], 2, 128, 4, 16, torch.bfloat16, seed=4, spare=spare)
     q = setup.queries(6, 8)
@@ -208,11 +208,11 @@ def test_extreme_ranges(bits, kind):
 
 
 def test_q_slices_scale_and_given_buffers():
-    setup = Setup([520, 64], 2, 128, 4, 32, torch.bfloat16, seed=8)
+    setup = Setup([1030, 64], 2, 128, 4, 32, torch.bfloat16, seed=8)
     fused = torch.randn((2, 3, 4 + 2 + 2, 128), generator=setup.gen).to(torch.bfloat16)
     q = fused[:, :, :4]
     out = torch.empty((2, 3, 4, 128), dtype=torch.bfloat16, device=DEV)
-    ws = torch.full((civic.quant_attention_workspace_bytes(setup.cache, 17, 2, 3, 4),), 0xFF, dtype=torch.uint8, device=DEV)
+    ws = torch.full((civic.quant_attention_workspace_bytes(setup.cache, 33, 2, 3, 4),), 0xFF, dtype=torch.uint8, device=DEV)
     got, lse = civic.civic_quant_attention(fused.to(DEV)[:, :, :4], setup.cache, 0, setup.table, setup.lens, scale=-0.2, out=out,
                                            workspace=ws)
     assert got is out and lse is None
@@ -274,7 +274,7 @@ def test_many_sequences_share_blocks_evenly():
     check(setup, q, out, lse, 0.125, True)
 
 
-@pytest.mark.parametrize("spare", [0, 20])  # short tables: a block per item; longer ones: shared items
+@pytest.mark.parametrize("spare", [0, 60])  # short tables: a block per item; longer ones: shared items
 def test_captured_and_replayed_with_new_lengths(spare):
     setup = Setup([200, 90], 2, 128, 4, 16, torch.bfloat16, seed=13, spare=spare)
     q = setup.queries(1, 8).to(DEV)
@@ -363,7 +363,7 @@ def test_wrong_shapes_devices_and_types_raise():
                dict(lse=torch.empty((1, 1, 4), device=DEV, dtype=torch.float64))):
         with pytest.raises(ValueError):
             call(**kw)
-    long_table = torch.zeros((1, 33), dtype=torch.int32, device=DEV)
+    long_table = torch.zeros((1, 65), dtype=torch.int32, device=DEV)
     with pytest.raises(civic.CivicError):
         call(table=long_table, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
     with pytest.raises(civic.CivicError):
