@@ -187,10 +187,12 @@ civic_status_t move_impl(const MoveCall& c, void* stream_)
     const unsigned warps = civic::kQuantThreads / 32;
     for (int l0 = 0; l0 < c.n_layers; l0 += civic::kMaxQuantLayers) {
         const int nl = c.n_layers - l0 < civic::kMaxQuantLayers ? c.n_layers - l0 : civic::kMaxQuantLayers;
+        p.wide32 = (p.seq_stride | p.token_stride | p.head_stride) % 32 == 0;
         for (int l = 0; l < nl; ++l) {
             p.wide[2 * l] = (char*)const_cast<void*>(c.k[l0 + l]);
             p.wide[2 * l + 1] = (char*)const_cast<void*>(c.v[l0 + l]);
             p.cache[l] = (char*)const_cast<void*>(c.cache[l0 + l]);
+            p.wide32 = p.wide32 && aligned(c.k[l0 + l], 32) && aligned(c.v[l0 + l], 32);
         }
         const dim3 grid((p.n_units + warps - 1) / warps, 2u * nl);
         CIVIC_CUDA_TRY(d.dtype == CIVIC_BF16

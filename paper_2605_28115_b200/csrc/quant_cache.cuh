@@ -12,13 +12,15 @@
 // together because attention needs both: one tile is one contiguous piece of 1.25 to 9 KB.
 //
 // Both kernels move bytes (writing reads 2 bytes a channel and writes 0.6 or 1.1); a warp takes one
-// tile of K or of V.  Lanes hold 8 channels of a pair of tokens: four lanes make a group, so minimum
-// and maximum take two shuffles, and a lane's 8 codes are whole words of the layout.
+// tile of K or of V.  In the writing one lanes hold 16 channels of a pair of tokens by 32-byte loads: with 8
+// channels (and two shuffles a group) the per-group arithmetic made it bound by instruction issue at
+// 4.5 TB/s.  The reading one holds 8.
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <type_traits>
 
 #include "index_check.cuh"
 #include "pdl.cuh"
@@ -76,6 +78,7 @@ struct QuantMoveParams {
     int32_t n_heads, tiles;            // tiles a sequence's rows can touch
     int32_t n_rows, wide_rows;         // rows per sequence at most; valid range of idx
     int32_t page_tiles, max_pages, n_pages;
+    int32_t wide32;                    // rows' pointers and strides are multiples of 32 bytes
     int32_t* check;                    // fault record or NULL
 };
 
@@ -147,31 +150,54 @@ struct Half16<__half> {
     static constexpr uint32_t kNan = 0x7E00u;
 };
 
-// ---- one row's 8 channels of a lane ----------------------------------------------------------------
+// ---- a lane's share of a row ------------------------------------------------------------------------
 
 struct Codes8 {
     uint32_t w[2];   // 8 bits: 4 codes each; 4 bits: w[0] holds all eight
     uint32_t param;  // {s, m} of the lane's group
 };
 
-// Quantises the lane's 8 channels; its group is the aligned quad of lanes it belongs to.
+// 16 channels, half a group; two neighbouring lanes hold a group.
+struct Row16 {
+    uint32_t x[8];
+};
+// 32 bytes at once need 32-byte alignment (`wide`: the host has looked at pointers and strides).
+__device__ __forceinline__ Row16 load_row16(const void* p, bool wide)
+{
+    Row16 r;
+    if (!wide) {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p)), b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+        return Row16{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+    }
+    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r.x[0]), "=r"(r.x[1]), "=r"(r.x[2]), "=r"(r.x[3]), "=r"(r.x[4]), "=r"(r.x[5]), "=r"(r.x[6]), "=r"(r.x[7])
+                 : "l"(p));
+    return r;
+}
+struct Codes16 {
+    uint32_t w[4];   // 8 bits: 4 codes each; 4 bits: w[0], w[1] hold eight each
+    uint32_t param;
+};
+
 template <typename T, int BITS>
-__device__ __forceinline__ Codes8 quantise8(const uint4& v)
+__device__ __forceinline__ Codes16 quantise16(const Row16& v)
 {
     using H = Half16<T>;
     constexpr float kTop = BITS == 4 ? 15.f : 255.f;
     constexpr float kInvTop = BITS == 4 ? 0x1.111110p-4f : 0x1.010100p-8f;  // 1 / L rounded down
-    uint32_t mn = H::min2(H::min2(v.x, v.y), H::min2(v.z, v.w));
-    uint32_t mx = H::max2(H::max2(v.x, v.y), H::max2(v.z, v.w));
-    mn = H::min2(mn, __byte_perm(mn, mn, 0x1032));
-    mx = H::max2(mx, __byte_perm(mx, mx, 0x1032));
-    uint32_t both = __byte_perm(mn, mx ^ 0x80008000u, 0x5410);  // {min, -max}: one minimum reduces both
+    uint32_t mn = v.x[0], mx = v.x[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        mn = H::min2(mn, v.x[i]);
+        mx = H::max2(mx, v.x[i]);
+    }
+    mx ^= 0x80008000u;  // {min, -max} in one word: a single minimum reduces both
+    uint32_t both = H::min2(__byte_perm(mn, mx, 0x5410), __byte_perm(mn, mx, 0x7632));
     both = H::min2(both, __shfl_xor_sync(0xFFFFFFFFu, both, 1));
-    both = H::min2(both, __shfl_xor_sync(0xFFFFFFFFu, both, 2));
     const float low = H::lo(both), range = -H::hi(both) - low;
     const bool finite = range <= 3.402823466e38f;  // false for NaN too
     const uint32_t sb = finite ? H::scale_bits(range, range * kInvTop, kTop) : H::kNan;
-    Codes8 r;
+    Codes16 r;
     r.param = finite ? (__byte_perm(both, sb, 0x1054)) : (H::kNan * 0x10001u);
     const float s = H::lo(sb);
     // 1 / s, never below it: the approximation is within one unit in the last place, one is added.  A
@@ -180,17 +206,24 @@ __device__ __forceinline__ Codes8 quantise8(const uint4& v)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
     inv = s > 0.f ? __uint_as_float(__float_as_uint(inv) + 1u) : 0.f;
     const float base = low - 0.5f * s;  // the 1/2 of the rounding
-    auto code = [&](float x) { return __float_as_uint(__fmaf_rd(x - base, inv, 8388608.f)); };  // floor in the low bits
-    const uint32_t c0 = code(H::lo(v.x)), c1 = code(H::hi(v.x)), c2 = code(H::lo(v.y)), c3 = code(H::hi(v.y));
-    const uint32_t c4 = code(H::lo(v.z)), c5 = code(H::hi(v.z)), c6 = code(H::lo(v.w)), c7 = code(H::hi(v.w));
+    uint32_t c[16];  // code in the low byte
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float x = (i & 1) ? H::hi(v.x[i >> 1]) : H::lo(v.x[i >> 1]);
+        c[i] = __float_as_uint(__fmaf_rd(x - base, inv, 8388608.f));  // floor in the low bits
+    }
     if constexpr (BITS == 4) {
-        const uint32_t b01 = __byte_perm(c0 + c1 * 16u, c2 + c3 * 16u, 0x0040);
-        const uint32_t b23 = __byte_perm(c4 + c5 * 16u, c6 + c7 * 16u, 0x0040);
-        r.w[0] = __byte_perm(b01, b23, 0x5410);
-        r.w[1] = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t b01 = __byte_perm(c[8 * h] + c[8 * h + 1] * 16u, c[8 * h + 2] + c[8 * h + 3] * 16u, 0x0040);
+            const uint32_t b23 = __byte_perm(c[8 * h + 4] + c[8 * h + 5] * 16u, c[8 * h + 6] + c[8 * h + 7] * 16u, 0x0040);
+            r.w[h] = __byte_perm(b01, b23, 0x5410);
+            r.w[2 + h] = 0;
+        }
     } else {
-        r.w[0] = __byte_perm(__byte_perm(c0, c1, 0x0040), __byte_perm(c2, c3, 0x0040), 0x5410);
-        r.w[1] = __byte_perm(__byte_perm(c4, c5, 0x0040), __byte_perm(c6, c7, 0x0040), 0x5410);
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            r.w[h] = __byte_perm(__byte_perm(c[4 * h], c[4 * h + 1], 0x0040), __byte_perm(c[4 * h + 2], c[4 * h + 3], 0x0040), 0x5410);
     }
     return r;
 }
@@ -252,8 +285,8 @@ template <typename T, int HD, int BITS>
 __global__ void __launch_bounds__(kQuantThreads) quant_write_kernel(const __grid_constant__ QuantMoveParams p)
 {
     using Tile = QuantTile<HD, BITS>;
-    constexpr int kLanesPerRow = HD / 8, kPairs = 8 * kLanesPerRow / 32;  // token pairs per lane
-    constexpr int kChunk = kPairs < 4 ? kPairs : 4;                       // of which this many are in flight
+    constexpr int kLanesPerRow = HD / 16, kPairs = 8 * kLanesPerRow / 32;  // token pairs per lane
+    constexpr int kChunk = kPairs < 2 ? kPairs : 2;                        // of which this many are in flight
     wait_for_prior_kernels();
     const int lane = threadIdx.x & 31;
     const uint32_t unit = blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
@@ -271,56 +304,62 @@ __global__ void __launch_bounds__(kQuantThreads) quant_write_kernel(const __grid
             row = -1;
         }
     }
-    const int sub = lane / kLanesPerRow, c = lane % kLanesPerRow, group = c >> 2, quad = c & 3;
-    const char* src = p.wide[blockIdx.y] + u.seq * p.seq_stride + u.head * p.head_stride + c * 16;
+    const int sub = lane / kLanesPerRow, c = lane % kLanesPerRow, group = c >> 1, part = c & 1;
+    const char* src = p.wide[blockIdx.y] + u.seq * p.seq_stride + u.head * p.head_stride + c * 32;
     uint32_t* codes = reinterpret_cast<uint32_t*>(u.tile + (is_v ? Tile::kVCodes : 0));
     uint32_t* params = reinterpret_cast<uint32_t*>(u.tile + (is_v ? Tile::kVParams : Tile::kKParams));
+    // with FULL all 16 rows are there
+    auto write = [&](auto full) {
+        constexpr bool FULL = decltype(full)::value;
 #pragma unroll
-    for (int i0 = 0; i0 < kPairs; i0 += kChunk) {
-        uint4 x[kChunk][2];
-        int r[kChunk][2];
+        for (int i0 = 0; i0 < kPairs; i0 += kChunk) {
+            Row16 x[kChunk][2];
+            int r[kChunk][2];
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i)
+            for (int i = 0; i < kChunk; ++i)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int token = 2 * ((i0 + i) * (8 / kPairs) + sub) + b;
-                r[i][b] = __shfl_sync(0xFFFFFFFFu, row, token);
-                x[i][b] = make_uint4(0, 0, 0, 0);
-                if (r[i][b] >= 0) x[i][b] = __ldcs(reinterpret_cast<const uint4*>(src + r[i][b] * p.token_stride));
-            }
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) {
-            const int pair = (i0 + i) * (8 / kPairs) + sub;
-            Codes8 q[2];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                q[b] = quantise8<T, BITS>(x[i][b]);
-                if (r[i][b] < 0) continue;
-                if (quad == 0) params[(2 * pair + b) * Tile::kGroups + group] = q[b].param;
-                if (!is_v) {
-                    uint32_t* at = codes + Tile::k_word(2 * pair + b, quad, group * (BITS / 4));
-                    if constexpr (BITS == 4) *at = q[b].w[0];
-                    else *reinterpret_cast<uint2*>(at) = make_uint2(q[b].w[0], q[b].w[1]);
+                for (int b = 0; b < 2; ++b) {
+                    const int token = 2 * ((i0 + i) * (8 / kPairs) + sub) + b;
+                    r[i][b] = __shfl_sync(0xFFFFFFFFu, row, token);
+                    x[i][b] = Row16{};
+                    if (FULL || r[i][b] >= 0) x[i][b] = load_row16(src + r[i][b] * p.token_stride, p.wide32);
                 }
-            }
-            if (is_v) {
-                // channels 8 quad + 0..3 belong to g = 2 quad, 4..7 to g = 2 quad + 1
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int vl = (2 * quad + e) * 4 + (pair & 3);
+            for (int i = 0; i < kChunk; ++i) {
+                const int pair = (i0 + i) * (8 / kPairs) + sub;
+                const bool got[2] = {FULL || r[i][0] >= 0, FULL || r[i][1] >= 0};
+                const Codes16 q[2] = {quantise16<T, BITS>(x[i][0]), quantise16<T, BITS>(x[i][1])};
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    if (!got[b]) continue;
+                    if (part == 0) params[(2 * pair + b) * Tile::kGroups + group] = q[b].param;
+                    if (is_v) continue;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {  // channels 8 (2 part + e) .. + 7 of the group
+                        uint32_t* at = codes + Tile::k_word(2 * pair + b, 2 * part + e, group * (BITS / 4));
+                        if constexpr (BITS == 4) *at = q[b].w[e];
+                        else *reinterpret_cast<uint2*>(at) = make_uint2(q[b].w[2 * e], q[b].w[2 * e + 1]);
+                    }
+                }
+                if (!is_v) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {  // channels 4 (4 part + e) .. + 3: g = 4 part + e
+                    const int vl = (4 * part + e) * 4 + (pair & 3);
 #pragma unroll
                     for (int h = 0; h < BITS / 4; ++h) {
                         uint32_t* at = codes + Tile::v_word(pair >> 2, vl, group * (BITS / 4) + h);
-                        const uint32_t wa = q[0].w[BITS == 4 ? 0 : e], wb = q[1].w[BITS == 4 ? 0 : e];
-                        const uint32_t w = __byte_perm(wa, wb, (BITS == 4 ? e : h) ? 0x7632 : 0x5410);
-                        if (r[i][0] >= 0 && r[i][1] >= 0) *at = w;
-                        else if (r[i][0] >= 0) *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
-                        else if (r[i][1] >= 0) *(reinterpret_cast<uint16_t*>(at) + 1) = (uint16_t)(w >> 16);
+                        const uint32_t wa = q[0].w[BITS == 4 ? e >> 1 : e], wb = q[1].w[BITS == 4 ? e >> 1 : e];
+                        const uint32_t w = __byte_perm(wa, wb, (BITS == 4 ? e & 1 : h) ? 0x7632 : 0x5410);
+                        if (got[0] && got[1]) *at = w;
+                        else if (got[0]) *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
+                        else if (got[1]) *(reinterpret_cast<uint16_t*>(at) + 1) = (uint16_t)(w >> 16);
                     }
                 }
             }
         }
-    }
+    };
+    if (__all_sync(0xFFFFFFFFu, row >= 0)) write(std::true_type{});
+    else write(std::false_type{});
 }
 
 // Cache -> rows, with the same split.  Rows at and behind a sequence's count are left as they were.

@@ -84,6 +84,8 @@ CASES = [  # layers, n_seq, seq_len, s_out, heads, dim, bits, page, layout, dtyp
     (1, 2, 90, 33, 5, 256, 4, 128, "fused", torch.bfloat16),
     (2, 1, 40, 31, 2, 256, 8, 16, "list", torch.float16),
     (1, 4, 200, 100, 8, 128, 4, 1024, "token", torch.float16),
+    (2, 2, 60, 45, 2, 128, 4, 16, "odd", torch.bfloat16),
+    (1, 2, 60, 45, 2, 64, 8, 16, "odd", torch.float16),
 ]
 
 
@@ -103,6 +105,9 @@ def test_compaction_writes_what_the_oracle_quantises_and_nothing_else(case):
         kd, vd = (x.transpose(2, 3).contiguous().to(DEV).transpose(2, 3) for x in (k, v))
     elif layout == "list":
         kd, vd = [x.to(DEV) for x in k], [x.to(DEV) for x in v]
+    elif layout == "odd":  # rows aligned to 16 bytes only
+        kd, vd = (torch.cat([torch.zeros_like(x[..., :8]), x], 4).to(DEV)[..., 8:] for x in (k, v))
+        assert kd.data_ptr() % 32 == 16 and kd.stride(3) % 16 == 8
     else:  # slices of one projection [.., 3 * heads, dim]
         both = torch.cat([torch.zeros_like(k), k, v], 3).to(DEV)
         kd, vd = both[..., heads : 2 * heads, :], both[..., 2 * heads :, :]
