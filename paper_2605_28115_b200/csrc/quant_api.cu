@@ -1,10 +1,12 @@
 // C ABI of the quantised K/V cache: host-side validation and launches of the kernels in
 // quant_cache.cuh and quant_attention.cuh.  See include/civic.h for the contract of every entry point.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
 #include "host.hpp"
 #include "quant_attention.cuh"
+#include "quant_attention_wide.cuh"
 #include "quant_cache.cuh"
 
 using namespace civic_host;
@@ -78,6 +80,8 @@ bool lists_overlap(const void* const* a, int na, size_t a_bytes, const void* con
             if (overlaps(a[i], a_bytes, b[j], b_bytes)) return true;
     return false;
 }
+
+constexpr int64_t kWideRows = 16;
 
 struct MoveCall {
     const void* const* k;  // wide tensors
@@ -249,6 +253,34 @@ civic_status_t launch_attention(civic::QuantAttnParams& p, unsigned items, cudaS
     g_launches.fetch_add(2, std::memory_order_relaxed);
     return CIVIC_OK;
 }
+template <int HD, int BITS>
+civic_status_t launch_attention_wide(civic::QuantAttnParams& p, unsigned row_blocks, cudaStream_t stream)
+{
+    using T = __nv_bfloat16;
+    const auto kernel = civic::quant_attention_wide_kernel<T, HD, BITS>;
+    constexpr size_t smem = civic::qw_smem_bytes<HD>();
+    static_assert(smem <= kMaxDynamicSmem, "two tiles of queries and two stages of K and V fit into shared memory");
+    static std::atomic<int> allowed[64];
+    const civic_status_t as = allow_dynamic_smem(kernel, smem, allowed);
+    if (as != CIVIC_OK) return as;
+    p.blocks = std::min(sm_count(), civic::kQwMaxBlocks);
+    p.status = (int32_t*)p.partial;
+    p.partial = (float*)((char*)p.partial + civic::kQwStatusBytes);
+    const bool pdl = programmatic();
+    CIVIC_CUDA_TRY(civic::launch(pdl, kernel, (unsigned)p.blocks, (unsigned)civic::kQwThreads, smem, stream, p));
+    CIVIC_CUDA_TRY(civic::launch(pdl, civic::quant_attention_wide_join_kernel<T, HD>,
+                                 dim3(row_blocks * (unsigned)p.n_heads * 8u, (unsigned)p.n_seq), (unsigned)(HD / 4 * 8), 0, stream, p));
+    g_launches.fetch_add(2, std::memory_order_relaxed);
+    return CIVIC_OK;
+}
+civic_status_t launch_attention_wide_dim(const civic_quant_desc_t& d, civic::QuantAttnParams& p, int64_t rows, cudaStream_t stream)
+{
+    const unsigned row_blocks = (unsigned)((rows + civic::kQwRows - 1) / civic::kQwRows);
+    if (d.head_dim == 64)
+        return d.bits == 4 ? launch_attention_wide<64, 4>(p, row_blocks, stream) : launch_attention_wide<64, 8>(p, row_blocks, stream);
+    return d.bits == 4 ? launch_attention_wide<128, 4>(p, row_blocks, stream) : launch_attention_wide<128, 8>(p, row_blocks, stream);
+}
+
 template <typename T, int HD, int NT>
 civic_status_t launch_attention_bits(int bits, civic::QuantAttnParams& p, unsigned items, cudaStream_t stream)
 {
@@ -278,6 +310,13 @@ civic_status_t check_attention(const civic_quant_desc_t* desc, int32_t n_seq, in
     return CIVIC_OK;
 }
 
+// Whether the call takes the tcgen05 kernels: bf16 only (the other kernels lose less where results have 11
+// bits), heads whose accumulators for 256 rows fit into tensor memory, and enough query rows.
+bool wide_rows(const civic_quant_desc_t& d, int32_t q_len, int32_t q_heads)
+{
+    return d.dtype == CIVIC_BF16 && d.head_dim <= 128 && (int64_t)q_len * (q_heads / d.n_heads) > kWideRows;
+}
+
 // Whether an item's tiles are few enough for one block.
 bool whole_items(const civic_quant_desc_t& d, int32_t max_pages)
 {
@@ -286,6 +325,8 @@ bool whole_items(const civic_quant_desc_t& d, int32_t max_pages)
 
 size_t attention_workspace(const civic_quant_desc_t& d, int32_t max_pages, int32_t q_len, int32_t q_heads)
 {
+    if (wide_rows(d, q_len, q_heads))
+        return civic::kQwStatusBytes + (size_t)2 * civic::kQwMaxBlocks * civic::qw_slot_floats(d.head_dim) * 4;
     if (whole_items(d, max_pages)) return 0;
     const int nt = attention_tiles(d.head_dim, (int64_t)q_len * (q_heads / d.n_heads));
     return round_up((size_t)2 * civic::kQaMaxBlocks * 8 * nt * (d.head_dim + 2) * 4, 256);
@@ -410,6 +451,7 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     const unsigned items = (unsigned)((rows + 8 * nt - 1) / (8 * nt) * d.n_heads);
     // a block's share of the tiles, of at least 148 blocks', is counted in 32 bits
     if ((double)n_seq * items * (p.capacity / civic::kQuantTile) > 148.0 * (1 << 30)) return CIVIC_ERR_UNSUPPORTED;
+    if (wide_rows(d, q_len, q_heads)) return launch_attention_wide_dim(d, p, rows, (cudaStream_t)stream);
     return d.dtype == CIVIC_BF16 ? launch_attention_dim<__nv_bfloat16>(d, nt, p, items, (cudaStream_t)stream)
                                  : launch_attention_dim<__half>(d, nt, p, items, (cudaStream_t)stream);
 }

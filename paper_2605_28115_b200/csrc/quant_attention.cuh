@@ -32,6 +32,7 @@
 #include <type_traits>
 
 #include "quant_cache.cuh"
+#include "tensor_core.cuh"
 
 namespace civic {
 
@@ -52,6 +53,7 @@ struct QuantAttnParams {
     char* out;                   // [n_seq, q_len, q_heads, HD]
     float* lse;                  // [n_seq, q_len, q_heads] or NULL
     float* partial;              // [2 * blocks][rows][HD + 2]
+    int32_t* status;             // [blocks], the wide kernel's
     int64_t q_seq, q_token, q_head;  // strides in bytes
     int32_t n_seq, q_len, q_heads, n_heads, group;
     int32_t causal;
@@ -204,12 +206,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
     return d;
 }
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) { return Half16<__half>::pack(lo, hi); }
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 template <int OFFSET>
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src)
 {

@@ -1,0 +1,847 @@
+// Attention over the quantised cache for many query rows of a K/V head (a prompt's chunk, drafted
+// tokens of wide groups), on the 5th-generation tensor cores.  Same operator as quant_attention.cuh;
+// rows = query tokens x query heads of the K/V head.
+//
+// With many rows the products outweigh the unpacking, so every code is turned into its value once
+// per block of 256 rows: eight warps read tiles, make fp16 numbers of them and lay them into shared
+// memory as tcgen05 operands; one warp issues the products; eight warps hold the softmax of two tiles
+// of 128 rows, one row per thread:
+//   producers  K', V' [128 tokens, HD], 128-byte swizzled; queries of the next item
+//   MMA        S_t = Q_t K'^T into tensor memory, t = 0, 1; then O_t += P_t V', P_t read from tensor memory
+//   softmax    maximum, exp2, P_t packed over S_t; O_t is rescaled only when a row's reference moved
+// While one tile's softmax runs the tensor cores work for the other one.
+//
+// fp16 operands, and scores without a rounding in them.  In the middle of its codes a group is
+//     k = s (c - 8) + (m + 8 s):
+// s has 8 bits and c - 8 at most 3 besides powers of two, so s (c - 8) IS an fp16.  The second part is the
+// same for the 32 channels of a group; it meets the group's sum of q in a product of depth 16 of its own,
+// both as two fp16 parts (22 bits).  An 8-bit code is two nibbles, 16 (h - 8) + (l - 8) + 136, and takes two
+// products.  (With k itself rounded to fp16 a dominant score was off by 1e-3.)  V is rounded to fp16, 11
+// bits, as the weights are.
+//
+// fp16's range is kept by powers of two: per query row, and per tile of 16 tokens for K (the largest
+// s of a tile is in [2^-9, 2^-8)) and V (the largest |v| in [2^-7, 2^-6)): then a code enters the
+// multiply-add as the fp16 subnormal that its bits are (code * 2^-24, s * 2^24 below 2^16), one instruction
+// for two values.  Where a tile's tokens differ by more than 2^5 (K) or 2^8 (V) in size every token has a
+// power of its own (the softmax then looks at every column's factors).
+// fp16 results have 11 bits themselves: for them quant_attention.cuh, which loses none of V's, is used.
+//
+// Work split and joining as in quant_attention.cuh, in units of 128 tokens; items are (sequence, K/V head,
+// block of 256 rows), and a block of rows has as many units as its last row sees.
+#pragma once
+#include "quant_attention.cuh"
+#include "tensor_core.cuh"
+
+namespace civic {
+
+constexpr int kQwBlock = 128;      // tokens per unit
+constexpr int kQwRows = 256;       // query rows per item: two tiles of 128
+constexpr int kQwProducers = 8;    // warps that unpack: one tile of 16 tokens each
+constexpr int kQwThreads = 32 * (8 + 1 + kQwProducers);
+constexpr int kQwMaxBlocks = 148;
+constexpr int kQwMinUnits = 2;
+constexpr float kQwDropped = -3e38f;  // exponent of a token that is left out
+
+struct QwItem {
+    int seq, head, row_block, block;   // block: the next unit of the item
+    int len, q_len, row_blocks, units; // units: of the item
+};
+
+__device__ __forceinline__ int qw_sees(const QuantAttnParams& p, int len, int q_len, int row)
+{
+    return p.causal ? min(max(len - q_len + row / p.group + 1, 0), len) : len;
+}
+__device__ __forceinline__ int qw_units(const QuantAttnParams& p, int len, int q_len, int row_block)
+{
+    const int last = min((row_block + 1) * kQwRows, q_len * p.group) - 1;
+    return (qw_sees(p, len, q_len, last) + kQwBlock - 1) / kQwBlock;
+}
+// Units of one head of a sequence.
+__device__ __forceinline__ long long qw_head_units(const QuantAttnParams& p, int len, int q_len)
+{
+    const int blocks = (q_len * p.group + kQwRows - 1) / kQwRows;
+    if (!p.causal) return (long long)blocks * ((len + kQwBlock - 1) / kQwBlock);
+    long long sum = 0;
+    for (int b = 0; b < blocks; ++b) sum += qw_units(p, len, q_len, b);
+    return sum;
+}
+__device__ __forceinline__ int qw_len(const QuantAttnParams& p, int s) { return min(max(__ldg(p.lens + s), 0), p.capacity); }
+__device__ __forceinline__ int qw_q_len(const QuantAttnParams& p, int s)
+{
+    return p.q_lens ? min(max(__ldg(p.q_lens + s), 0), p.q_len) : p.q_len;
+}
+// Units of the whole call and of the sequences before `upto`; by a whole warp.
+__device__ __forceinline__ long long qw_total(const QuantAttnParams& p, int upto, long long& before)
+{
+    const int lane = threadIdx.x & 31;
+    long long total = 0, b = 0;
+    for (int s = lane; s < p.n_seq; s += 32) {
+        const long long u = qw_head_units(p, qw_len(p, s), qw_q_len(p, s)) * p.n_heads;
+        total += u;
+        if (s < upto) b += u;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        total += __shfl_xor_sync(0xFFFFFFFFu, total, d);
+        b += __shfl_xor_sync(0xFFFFFFFFu, b, d);
+    }
+    before = b;
+    return total;
+}
+__host__ __device__ inline long long qw_share(long long total, int blocks)
+{
+    const long long even = (total + blocks - 1) / blocks;
+    return even < kQwMinUnits ? kQwMinUnits : even;
+}
+
+// The item of sequence `seq`, head and row block given; its first unit.
+__device__ __forceinline__ void qw_enter(const QuantAttnParams& p, QwItem& it)
+{
+    it.units = uniform(qw_units(p, it.len, it.q_len, it.row_block));
+}
+__device__ __forceinline__ void qw_enter_sequence(const QuantAttnParams& p, QwItem& it)
+{
+    it.len = uniform(qw_len(p, it.seq));
+    it.q_len = uniform(qw_q_len(p, it.seq));
+    it.row_blocks = uniform((it.q_len * p.group + kQwRows - 1) / kQwRows);
+}
+// To the next item that has units; false behind the last one.
+__device__ __forceinline__ bool qw_next(const QuantAttnParams& p, QwItem& it)
+{
+    it.block = 0;
+    for (;;) {
+        if (++it.row_block >= it.row_blocks) {
+            it.row_block = 0;
+            if (it.row_blocks == 0 || ++it.head >= p.n_heads) {
+                it.head = 0;
+                if (++it.seq >= p.n_seq) return false;
+                qw_enter_sequence(p, it);
+                if (it.row_blocks == 0) continue;
+            }
+        }
+        qw_enter(p, it);
+        if (it.units > 0) return true;
+    }
+}
+__device__ __forceinline__ QwItem qw_locate(const QuantAttnParams& p, long long unit)
+{
+    const int lane = threadIdx.x & 31;
+    QwItem it;
+    it.seq = it.head = it.row_block = it.block = it.len = it.q_len = it.row_blocks = it.units = 0;
+    long long before = 0;
+    for (int s0 = 0; s0 < p.n_seq; s0 += 32) {
+        const int s = s0 + lane;
+        const long long per_head = s < p.n_seq ? qw_head_units(p, qw_len(p, s), qw_q_len(p, s)) : 0;
+        const long long u = per_head * p.n_heads, upto = before + warp_scan_add(u, lane);
+        const unsigned past = __ballot_sync(0xFFFFFFFFu, upto > unit);
+        if (past) {
+            const int l = __ffs(past) - 1;
+            long long rest = unit - __shfl_sync(0xFFFFFFFFu, upto - u, l);
+            const long long head_units = __shfl_sync(0xFFFFFFFFu, per_head, l);
+            it.seq = uniform(s0 + l);
+            qw_enter_sequence(p, it);
+            it.head = uniform((int)(rest / head_units));
+            rest -= it.head * head_units;
+            for (;; ++it.row_block) {
+                qw_enter(p, it);
+                if (rest < it.units) break;
+                rest -= it.units;
+            }
+            it.block = uniform((int)rest);
+            return it;
+        }
+        before = __shfl_sync(0xFFFFFFFFu, upto, 31);
+    }
+    return it;
+}
+
+// fp16 x fp16 -> fp32, M = 128
+__host__ __device__ constexpr uint32_t qw_idesc(int n, int b_mn_major)
+{
+    return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+struct QwStage {                     // beside a V' stage
+    float k_factor[kQwBlock];        // 2^e of the token's K'
+    float v_exp[kQwBlock];           // e of its V', kQwDropped for a token that is left out
+    int per_token[kQwProducers];     // tile's tokens have factors of their own
+};
+struct QwSync {
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full;
+    uint64_t s_full[2], p_ready[2], o_done[2], drained;
+    float row_factor[2][kQwRows];    // per item (alternating) and row: takes raw scores to base-2 logits
+    QwStage stage[2];
+    uint32_t params[kQwProducers][2][kQuantTile * 4];  // per producer warp, K | V: {s, m} as fp16, [token][group]
+    uint32_t tmem_base;
+    int abort;
+};
+
+// q [2 tiles][128 rows] | k [2 stages, in 8 bits 2 parts][128 tokens] | v [2 stages][128 tokens], blocks of
+// 64 columns | sums of q [2 tiles][128 x 16], groups' middles [2 stages][128 x 16]
+constexpr int kQwMidBytes = 128 * 16 * 2;
+template <int HD>
+__host__ __device__ constexpr size_t qw_smem_bytes()
+{
+    return (size_t)(2 + 2 + 2) * (HD / 64) * 16384 + 4 * kQwMidBytes + sizeof(QwSync) + 1024;
+}
+// Byte of group j's four depths of row r in such a [128 x 16] operand: 8 rows x 16 bytes are contiguous
+__device__ __forceinline__ int qw_mid_at(int r, int j) { return (r >> 3) * 256 + (j >> 1) * 128 + (r & 7) * 16 + (j & 1) * 8; }
+// and its descriptor: no swizzle, 128 bytes from one half of the depth to the other, 256 between groups of 8 rows
+__device__ __forceinline__ uint64_t qw_mid_desc(uint32_t smem_addr)
+{
+    return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 16 | (uint64_t)(256 >> 4) << 32 | 1ull << 46;
+}
+// Workspace: status word of every block | slots of partial rows, two per block: O [256][HD], {m, l} [256]
+constexpr size_t kQwStatusBytes = 1024;
+__host__ __device__ constexpr size_t qw_slot_floats(int hd) { return (size_t)kQwRows * (hd + 2); }
+
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// Floor of log2, within -100 .. 119 (larger numbers overflow fp16 and end as NaN).
+__device__ __forceinline__ int qw_log2(float x) { return min(max((int)(__float_as_uint(x) >> 23) - 127, -100), 119); }
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+
+// Both functions prepare one tile's scales and minima for the fp16 arithmetic, by a warp: lane = (token
+// lane / 2, every second group from lane % 2 on).  They return the exponent of the lane's token.
+
+// V: {s 2^24, m} 2^-e.  With clear_nan a NaN group becomes zeros (and `nan` tells the lane's token).
+template <typename T, int HD, int BITS>
+__device__ __forceinline__ int qw_params_v(const uint32_t (&from)[HD / 64], uint32_t* to, bool have, bool clear_nan, bool& per_token, bool& nan)
+{
+    using H = Half16<T>;
+    constexpr int NG = HD / 32;
+    const int lane = threadIdx.x & 31, token = lane >> 1, first = lane & 1;
+    float s[NG / 2], m[NG / 2], mag = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < NG / 2; ++i) {
+        const uint32_t w = have ? from[i] : 0u;
+        s[i] = H::lo(w);
+        m[i] = H::hi(w);
+        bad |= m[i] != m[i];
+        mag = fmaxf(mag, fmaxf(fabsf(m[i]), fabsf(fmaf(s[i], BITS == 4 ? 15.f : 255.f, m[i]))));
+    }
+    mag = fmaxf(mag, __shfl_xor_sync(0xFFFFFFFFu, mag, 1));
+    float most = mag;
+#pragma unroll
+    for (int d = 2; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+    const bool uneven = __any_sync(0xFFFFFFFFu, mag > 0.f && mag < most * 0x1p-8f);
+    const bool other_bad = __shfl_xor_sync(0xFFFFFFFFu, (int)bad, 1) != 0;  // every lane takes part
+    bad = bad || other_bad;
+    nan = clear_nan && bad;
+    const bool some_nan = __any_sync(0xFFFFFFFFu, nan);
+    per_token = uneven || some_nan;
+    const int e = qw_log2(uneven ? mag : most) + 7;
+    const float down = pow2(-e), down24 = down * 0x1p24f;
+#pragma unroll
+    for (int i = 0; i < NG / 2; ++i) to[token * NG + first + 2 * i] = nan ? 0u : pack_half2(s[i] * down24, m[i] * down);
+    return e;
+}
+
+// K: {s 2^24, -8 s} 2^-e, and the middles m + 8 s (m + 136 s) 2^(8 - e) as two fp16, each twice, into row
+// `line` of `mid`.
+template <typename T, int HD, int BITS>
+__device__ __forceinline__ int qw_params_k(const uint32_t (&from)[HD / 64], uint32_t* to, uint8_t* mid, int line0, bool have,
+                                           bool& per_token)
+{
+    using H = Half16<T>;
+    constexpr int NG = HD / 32;
+    const int lane = threadIdx.x & 31, token = lane >> 1, first = lane & 1;
+    float s[NG / 2], m[NG / 2], s_max = 0.f, mag = 0.f;
+#pragma unroll
+    for (int i = 0; i < NG / 2; ++i) {
+        const uint32_t w = have ? from[i] : 0u;
+        s[i] = H::lo(w);
+        m[i] = fmaf(s[i], BITS == 4 ? 8.f : 136.f, H::hi(w));
+        s_max = fmaxf(s_max, s[i]);
+        mag = fmaxf(mag, fabsf(m[i]));
+    }
+    // 2^e above s_max * 2^8 and above mag * 2^-7: the scales stay below 2^-8, the middles below 2^15
+    float size = fmaxf(s_max * 0x1p9f, mag * 0x1p-6f);
+    size = fmaxf(size, __shfl_xor_sync(0xFFFFFFFFu, size, 1));
+    float most = size;
+#pragma unroll
+    for (int d = 2; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+    per_token = __any_sync(0xFFFFFFFFu, size > 0.f && size < most * 0x1p-5f);
+    const int e = qw_log2(per_token ? size : most);
+    const float down = pow2(-e), down24 = down * 0x1p24f, down8 = down * 0x1p8f;
+#pragma unroll
+    for (int i = 0; i < NG / 2; ++i) {
+        const int j = first + 2 * i;
+        to[token * NG + j] = pack_half2(s[i] * down24, s[i] * down * -8.f);
+        const float x = m[i] * down8;
+        const uint32_t h = pack_half2(x, x);
+        const float rest = x - Half16<__half>::lo(h);
+        *reinterpret_cast<uint2*>(mid + qw_mid_at(line0 + token, j)) = make_uint2(h, pack_half2(rest, rest));
+        if constexpr (NG == 2) *reinterpret_cast<uint2*>(mid + qw_mid_at(line0 + token, j + 2)) = make_uint2(0u, 0u);
+    }
+    return e;
+}
+
+template <typename T, int HD, int BITS>
+__global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(const __grid_constant__ QuantAttnParams p)
+{
+    using Tile = QuantTile<HD, BITS>;
+    constexpr int NG = Tile::kGroups, DB = HD / 64;
+    constexpr int kTileBytes = DB * 16384;  // one operand of 128 rows
+    constexpr int kParts = BITS / 4;        // of K'
+    constexpr int kKStages = 2 / kParts;
+    extern __shared__ uint8_t qw_smem[];
+    uint8_t* base = qw_smem + ((1024u - (smem_u32(qw_smem) & 1023u)) & 1023u);
+    uint8_t* q_sm = base;
+    uint8_t* k_sm = q_sm + 2 * kTileBytes;
+    uint8_t* v_sm = k_sm + 2 * kTileBytes;
+    uint8_t* q_mid = v_sm + 2 * kTileBytes;
+    uint8_t* k_mid = q_mid + 2 * kQwMidBytes;
+    QwSync& sy = *reinterpret_cast<QwSync*>(k_mid + 2 * kQwMidBytes);
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    volatile int* abort = &sy.abort;
+    int* status = p.status + blockIdx.x;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sy.k_full[i], kQwProducers);
+            mbar_init(&sy.v_full[i], kQwProducers);
+            mbar_init(&sy.k_empty[i], 1);
+            mbar_init(&sy.v_empty[i], 1);
+            mbar_init(&sy.s_full[i], 1);
+            mbar_init(&sy.p_ready[i], 4);
+            mbar_init(&sy.o_done[i], 1);
+        }
+        mbar_init(&sy.q_full, kQwProducers);
+        mbar_init(&sy.drained, 1);
+        sy.abort = 0;
+        fence_barrier_init();
+    }
+    if (warp == 8) tmem_alloc(&sy.tmem_base, 512);
+    release_next_kernel();
+    wait_for_prior_kernels();
+    if (threadIdx.x == 0) *status = 0;
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = sy.tmem_base;  // S_0, S_1 at columns 0 and 128 (P over their first halves), O_0, O_1 at 256 and 384
+
+    long long unused;
+    const long long total = qw_total(p, 0, unused), share = qw_share(total, p.blocks);
+    const long long begin = blockIdx.x * share;
+    const int units = uniform((int)max(min(share, total - begin), 0LL));
+    QwItem it;
+    if (units > 0) it = qw_locate(p, begin);
+    auto wait = [&](uint64_t* bar, uint32_t parity, int code) {
+        return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort, status, code)) != 0;
+    };
+
+    if (warp >= 9 && units > 0) {
+        // ---- producers: warp pw takes tile pw of each block of 128 tokens
+        const int pw = warp - 9, g = lane >> 2, t = lane & 3;
+        const int row = (g >> 1) + 4 * (g & 1);  // K rows of a quarter of the warp: 4 apart, so that its stores hit all banks
+        const int64_t page_stride = (int64_t)p.n_heads * p.page_tiles * Tile::kBytes;
+        uint32_t* kp = sy.params[pw][0];
+        uint32_t* vp = sy.params[pw][1];
+        QwItem nx = it;         // the block whose tile is in registers
+        int left = units;       // blocks from it on
+        // one tile's codes, fetched a block ahead
+        uint32_t kw[2][Tile::kWords], vw[2][Tile::kWords], k_par[NG / 2], v_par[NG / 2];
+        const char* tile = nullptr;  // NULL: no token of the tile is there
+        bool found = true;           // its page exists
+        auto fetch = [&]() {
+            const int n = nx.block * 8 + pw;
+            tile = nullptr;
+            found = true;
+            if (n * kQuantTile >= nx.len) return;
+            const int slot = p.page_magic ? (int)__umulhi((uint32_t)n, p.page_magic) : n;
+            const int page = __ldg(p.block_table + (size_t)nx.seq * p.max_pages + slot);
+            if ((uint32_t)page >= (uint32_t)p.n_pages) {
+                found = false;
+                if (p.check && lane == 0) report_bad_index(p.check, kIndexBadPage, nx.seq, slot, page);
+                return;
+            }
+            tile = p.cache + page * page_stride + ((int64_t)nx.head * p.page_tiles + (n - slot * p.page_tiles)) * Tile::kBytes;
+            const uint32_t* kc = reinterpret_cast<const uint32_t*>(tile);
+            const uint32_t* vc = reinterpret_cast<const uint32_t*>(tile + Tile::kVCodes);
+#pragma unroll
+            for (int i = 0; i < NG / 2; ++i) {
+                const int at = (lane >> 1) * NG + (lane & 1) + 2 * i;
+                k_par[i] = __ldg(reinterpret_cast<const uint32_t*>(tile + Tile::kKParams) + at);
+                v_par[i] = __ldg(reinterpret_cast<const uint32_t*>(tile + Tile::kVParams) + at);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int pl = 0; pl < Tile::kPlanes; ++pl) {
+                    const uint32_t* ka = kc + Tile::k_word(row + 8 * h, t, pl * Tile::kPlane);
+                    const uint32_t* va = vc + Tile::v_word(h, lane, pl * Tile::kPlane);
+                    if constexpr (Tile::kPlane == 4) {
+                        const uint4 a = __ldg(reinterpret_cast<const uint4*>(ka)), b = __ldg(reinterpret_cast<const uint4*>(va));
+                        kw[h][4 * pl] = a.x; kw[h][4 * pl + 1] = a.y; kw[h][4 * pl + 2] = a.z; kw[h][4 * pl + 3] = a.w;
+                        vw[h][4 * pl] = b.x; vw[h][4 * pl + 1] = b.y; vw[h][4 * pl + 2] = b.z; vw[h][4 * pl + 3] = b.w;
+                    } else {
+                        const uint2 a = __ldg(reinterpret_cast<const uint2*>(ka)), b = __ldg(reinterpret_cast<const uint2*>(va));
+                        kw[h][0] = a.x; kw[h][1] = a.y;
+                        vw[h][0] = b.x; vw[h][1] = b.y;
+                    }
+                }
+        };
+        fetch();
+        bool ok = true;
+        for (int u = 0, seg = 0; ok && u < units; ++seg) {
+            // the item's queries, once the products of the previous item's scores are done
+            if (u > 0 && !(ok = wait(&sy.k_empty[(u - 1) % kKStages], ((u - 1) / kKStages) & 1, kAggTimeoutEmpty))) break;
+            const int n_blocks = min(units - u, it.units - it.block), n_rows = it.q_len * p.group - it.row_block * kQwRows;
+            const int seen_by_all = qw_sees(p, it.len, it.q_len, it.row_block * kQwRows);
+#pragma unroll 1
+            for (int pass = 0; pass < 4; ++pass) {
+                const int r = pw * 32 + pass * 8 + g;  // row of the item
+                if (pw >= 4 && n_rows <= 128) break;
+                const int grow = it.row_block * kQwRows + r, token = grow / p.group, sub = grow - token * p.group;
+                float f[NG][8], top = 0.f;
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    uint4 x = make_uint4(0, 0, 0, 0);
+                    if (r < n_rows)
+                        x = __ldg(reinterpret_cast<const uint4*>(p.q + it.seq * p.q_seq + token * p.q_token +
+                                                                 (it.head * p.group + sub) * p.q_head + (j * 32 + t * 8) * 2));
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        f[j][i] = (i & 1) ? Half16<T>::hi(w[i >> 1]) : Half16<T>::lo(w[i >> 1]);
+                        top = fmaxf(top, fabsf(f[j][i]));
+                    }
+                }
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 126);
+                const float up = p.scale_log2e < 0.f ? -pow2(14 - e) : pow2(14 - e);  // factors are not negative then
+                if (t == 0) sy.row_factor[seg & 1][r] = pow2(e - 14) * fabsf(p.scale_log2e);
+                uint8_t* at = q_sm + (r >> 7) * kTileBytes + (r & 127) * 128;
+                float mine = 0.f;  // sum over group t
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        f[j][i] *= up;
+                        sum += f[j][i];
+                    }
+                    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+                    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                    if (t == j) mine = sum * 0x1p-8f;
+                    // channels in the order in which the codes come out of a word
+                    const uint4 v = BITS == 4
+                                        ? make_uint4(pack_half2(f[j][0], f[j][4]), pack_half2(f[j][1], f[j][5]),
+                                                     pack_half2(f[j][2], f[j][6]), pack_half2(f[j][3], f[j][7]))
+                                        : make_uint4(pack_half2(f[j][0], f[j][2]), pack_half2(f[j][1], f[j][3]),
+                                                     pack_half2(f[j][4], f[j][6]), pack_half2(f[j][5], f[j][7]));
+                    *reinterpret_cast<uint4*>(at + (j >> 1) * 16384 + (((4 * (j & 1) + t) ^ (r & 7)) << 4)) = v;
+                }
+                const float high = Half16<__half>::lo(pack_half2(mine, 0.f));
+                const uint32_t both = pack_half2(high, mine - high);
+                *reinterpret_cast<uint2*>(q_mid + (r >> 7) * kQwMidBytes + qw_mid_at(r & 127, t)) = make_uint2(both, both);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sy.q_full);
+            for (int b = 0; b < n_blocks; ++b, ++u) {
+                const int st = u & 1, phase = (u >> 1) & 1, pos = (nx.block * 8 + pw) * kQuantTile;
+                const int k_st = u % kKStages, k_phase = (u / kKStages) & 1;
+                const bool mixed = (nx.block + 1) * kQwBlock > seen_by_all;  // some row does not see all of the block
+                const bool have = tile != nullptr && pos + (lane >> 1) < nx.len;
+                bool per_token_k, per_token_v, nan_v;
+                // ---- K'
+                if (!(ok = wait(&sy.k_empty[k_st], k_phase ^ 1, kAggTimeoutEmpty))) break;
+                const int ek = qw_params_k<T, HD, BITS>(k_par, kp,
+                                                        k_mid + k_st * kQwMidBytes, pw * 16, have, per_token_k);
+                // a NaN of V would reach rows that do not see its token through 0 * NaN: it is sent through the
+                // token's factor instead, which only the rows that see it use
+                const int ev = qw_params_v<T, HD, BITS>(v_par, vp, have, mixed,
+                                                        per_token_v, nan_v);
+                __syncwarp();
+                uint8_t* k_at = k_sm + k_st * kTileBytes;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = row + 8 * h, line = pw * 16 + r;
+                    uint8_t* at = k_at + line * 128;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) {
+                        const uint32_t par = kp[r * NG + j];
+                        const uint32_t s = __byte_perm(par, par, 0x1010), n8 = __byte_perm(par, par, 0x3232);
+                        uint8_t* to = at + (j >> 1) * 16384 + (((4 * (j & 1) + t) ^ (r & 7)) << 4);
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if constexpr (BITS == 4) {
+                            if (tile) {
+                                const uint32_t x = kw[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);  // s / 16
+                                v = make_uint4(hfma2(x & 0x000F000Fu, s, n8), hfma2(x & 0x00F000F0u, s16, n8),
+                                               hfma2(y & 0x000F000Fu, s, n8), hfma2(y & 0x00F000F0u, s16, n8));
+                            }
+                        } else {
+                            uint4 high = make_uint4(0, 0, 0, 0);
+                            if (tile) {
+                                const uint32_t x = kw[h][2 * j], y = kw[h][2 * j + 1], n128 = hmul2(n8, 0x4C004C00u);  // times 16
+                                v = make_uint4(hfma2(x & 0x000F000Fu, s, n8), hfma2((x >> 8) & 0x000F000Fu, s, n8),
+                                               hfma2(y & 0x000F000Fu, s, n8), hfma2((y >> 8) & 0x000F000Fu, s, n8));
+                                high = make_uint4(hfma2(x & 0x00F000F0u, s, n128), hfma2((x >> 8) & 0x00F000F0u, s, n128),
+                                                  hfma2(y & 0x00F000F0u, s, n128), hfma2((y >> 8) & 0x00F000F0u, s, n128));
+                            }
+                            *reinterpret_cast<uint4*>(to + kTileBytes) = high;
+                        }
+                        *reinterpret_cast<uint4*>(to) = v;
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sy.k_full[k_st]);
+                // ---- V' and the tokens' factors
+                if (!(ok = wait(&sy.v_empty[st], phase ^ 1, kAggTimeoutEmpty))) break;
+                QwStage& stage = sy.stage[st];
+                if ((lane & 1) == 0) {
+                    const int c = pw * 16 + (lane >> 1);
+                    stage.k_factor[c] = nan_v ? __int_as_float(0x7FC00000) : pow2(ek);
+                    stage.v_exp[c] = found ? (float)ev : kQwDropped;
+                }
+                if (lane == 0) stage.per_token[pw] = per_token_k || per_token_v;
+                uint8_t* v_at = v_sm + st * kTileBytes;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int ra = 8 * h + 2 * t, rb = ra + 1;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) {
+                        const uint32_t pa = vp[ra * NG + j], pb = vp[rb * NG + j];
+                        const uint32_t s = __byte_perm(pa, pb, 0x5410), m = __byte_perm(pa, pb, 0x7632);
+                        uint32_t c[4] = {0u, 0u, 0u, 0u};  // channel n of both tokens
+                        if (tile) {
+                            if constexpr (BITS == 4) {
+                                const uint32_t x = vw[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);
+                                c[0] = hfma2(x & 0x000F000Fu, s, m);
+                                c[1] = hfma2(x & 0x00F000F0u, s16, m);
+                                c[2] = hfma2(y & 0x000F000Fu, s, m);
+                                c[3] = hfma2(y & 0x00F000F0u, s16, m);
+                            } else {
+                                const uint32_t x = vw[h][2 * j], y = vw[h][2 * j + 1];
+                                c[0] = hfma2(x & 0x00FF00FFu, s, m);
+                                c[1] = hfma2((x >> 8) & 0x00FF00FFu, s, m);
+                                c[2] = hfma2(y & 0x00FF00FFu, s, m);
+                                c[3] = hfma2((y >> 8) & 0x00FF00FFu, s, m);
+                            }
+                        }
+                        const int chunk = 4 * (j & 1) + (g >> 1), off = (j >> 1) * 16384 + (g & 1) * 8;
+                        const int la = pw * 16 + ra, lb = la + 1;
+                        *reinterpret_cast<uint2*>(v_at + off + la * 128 + ((chunk ^ (ra & 7)) << 4)) =
+                            make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
+                        *reinterpret_cast<uint2*>(v_at + off + lb * 128 + ((chunk ^ (rb & 7)) << 4)) =
+                            make_uint2(__byte_perm(c[0], c[1], 0x7632), __byte_perm(c[2], c[3], 0x7632));
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sy.v_full[st]);
+                if (--left > 0) {
+                    if (++nx.block >= nx.units) qw_next(p, nx);
+                    fetch();
+                }
+            }
+            if (ok && u < units) qw_next(p, it);
+        }
+    } else if (warp == 8 && units > 0) {
+        // ---- MMA issue; the whole warp walks the loops in step, one elected lane issues
+        auto uni = [](uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); };
+        const uint64_t desc_q = umma_desc(smem_u32(q_sm), 16, 1024), desc_k = umma_desc(smem_u32(k_sm), 16, 1024);
+        const uint64_t desc_v = umma_desc(smem_u32(v_sm), 16384, 1024);
+        const uint64_t desc_qm = qw_mid_desc(smem_u32(q_mid)), desc_km = qw_mid_desc(smem_u32(k_mid));
+        const uint32_t hi_m = (uint32_t)(desc_qm >> 32);
+        const uint32_t hi_q = (uint32_t)(desc_q >> 32), hi_k = (uint32_t)(desc_k >> 32), hi_v = (uint32_t)(desc_v >> 32);
+        auto desc = [](uint32_t hi, uint32_t lo) { return ((uint64_t)hi << 32) | lo; };
+        constexpr uint32_t idesc_s = qw_idesc(kQwBlock, 0), idesc_o = qw_idesc(HD, 1);
+        auto scores = [&](int t, int st) {
+            const uint32_t d = uni(tmem + 128u * t), a0 = uni((uint32_t)desc_q + (uint32_t)((t * kTileBytes) >> 4));
+            const uint32_t b0 = uni((uint32_t)desc_k + (uint32_t)((st * kTileBytes) >> 4));
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) {
+                const uint32_t step = (uint32_t)(kk >> 2) * 1024u + 2u * (uint32_t)(kk & 3);
+#pragma unroll
+                for (int part = 0; part < kParts; ++part)
+                    if (elect_one())
+                        umma_bf16(d, desc(hi_q, a0 + step), desc(hi_k, b0 + step + (uint32_t)(part * (kTileBytes >> 4))), idesc_s,
+                                  (kk | part) != 0);
+            }
+            const uint32_t am = uni((uint32_t)desc_qm + (uint32_t)((t * kQwMidBytes) >> 4));
+            const uint32_t bm = uni((uint32_t)desc_km + (uint32_t)((st * kQwMidBytes) >> 4));
+            if (elect_one()) umma_bf16(d, desc(hi_m, am), desc(hi_m, bm), idesc_s, 1);
+            if (elect_one()) umma_commit(&sy.s_full[t]);
+            __syncwarp();
+        };
+        bool ok = true;
+        int done[2] = {0, 0};  // blocks whose weights have been waited for, per tile of rows
+        for (int u = 0, seg = 0; ok && u < units; ++seg) {
+            const int n_blocks = min(units - u, it.units - it.block);
+            const int tiles = it.q_len * p.group - it.row_block * kQwRows > 128 ? 2 : 1;
+            if (!(ok = wait(&sy.q_full, seg & 1, kAggTimeoutFull))) break;
+            if (!(ok = wait(&sy.k_full[u % kKStages], (u / kKStages) & 1, kAggTimeoutFull))) break;
+            tc_fence_after_sync();
+            for (int t = 0; t < tiles; ++t) scores(t, u % kKStages);
+            if (elect_one()) umma_commit(&sy.k_empty[u % kKStages]);
+            __syncwarp();
+            for (int b = 0; ok && b < n_blocks; ++b, ++u) {
+                const int st = u & 1, k_next = (u + 1) % kKStages, k_next_phase = ((u + 1) / kKStages) & 1;
+                const bool more = b + 1 < n_blocks;
+                for (int t = 0; t < tiles; ++t) {
+                    if (!(ok = wait(&sy.p_ready[t], done[t] & 1, kAggTimeoutAcc))) break;
+                    ++done[t];
+                    if (t == 0 && !(ok = wait(&sy.v_full[st], (u >> 1) & 1, kAggTimeoutFull))) break;
+                    tc_fence_after_sync();
+                    const uint32_t d = uni(tmem + 256u + 128u * t), a = uni(tmem + 128u * t);
+                    const uint32_t b0 = uni((uint32_t)desc_v + (uint32_t)((st * kTileBytes) >> 4));
+                    const uint32_t keep = uni(b > 0);
+#pragma unroll
+                    for (int kk = 0; kk < kQwBlock / 16; ++kk)
+                        if (elect_one()) umma_bf16_a_tmem(d, a + 8u * kk, desc(hi_v, b0 + 128u * kk), idesc_o, kk != 0 ? 1u : keep);
+                    if (!more && elect_one()) umma_commit(&sy.o_done[t]);
+                    __syncwarp();
+                    if (more) {
+                        if (t == 0 && !(ok = wait(&sy.k_full[k_next], k_next_phase, kAggTimeoutFull))) break;
+                        tc_fence_after_sync();
+                        scores(t, k_next);
+                    }
+                }
+                if (!ok) break;
+                if (elect_one()) {
+                    umma_commit(&sy.v_empty[st]);
+                    if (more) umma_commit(&sy.k_empty[k_next]);
+                }
+                __syncwarp();
+            }
+            if (ok && u < units) qw_next(p, it);
+        }
+        // whatever is still in flight, after a time-out too, ends before the tensor memory goes
+        if (elect_one()) umma_commit(&sy.drained);
+        __syncwarp();
+        const long long t0 = clock64();
+        while (!mbar_try_wait(&sy.drained, 0) && (unsigned long long)(clock64() - t0) < (1ull << 24)) {}
+    } else if (warp < 8 && units > 0) {
+        // ---- softmax: thread = row 32 * (warp % 4) + lane of tile warp / 4
+        const int t = warp >> 2, quarter = warp & 3, r = t * 128 + quarter * 32 + lane;
+        const uint32_t tm_s = tmem + ((uint32_t)(quarter * 32) << 16) + 128u * t, tm_o = tm_s + 256u;
+        int turn = 0, items = 0;  // blocks and items of this tile so far
+        bool ok = true;
+        for (int u = 0, seg = 0; ok && u < units; ++seg) {
+            const int n_blocks = min(units - u, it.units - it.block);
+            const int row0 = it.row_block * kQwRows, n_rows = it.q_len * p.group - row0;
+            if (t == 1 && n_rows <= 128) {
+                u += n_blocks;
+                if (u < units) qw_next(p, it);
+                continue;
+            }
+            const int sees = r < n_rows ? qw_sees(p, it.len, it.q_len, row0 + r) : it.len;
+            const int seen_by_all = uniform(qw_sees(p, it.len, it.q_len, row0));
+            float ref = 0.f, l = 0.f, factor = 0.f;
+            for (int b = 0; b < n_blocks; ++b, ++u, ++turn) {
+                const int st = u & 1, pos = (it.block + b) * kQwBlock;
+                if (!(ok = wait(&sy.s_full[t], turn & 1, kAggTimeoutAcc))) break;
+                if (!(ok = wait(&sy.v_full[st], (u >> 1) & 1, kAggTimeoutFull))) break;  // for the factors
+                tc_fence_after_sync();
+                if (b == 0) factor = sy.row_factor[seg & 1][r];
+                const QwStage& stage = sy.stage[st];
+                const bool masked = pos + kQwBlock > seen_by_all;
+                // ---- the row's largest logit, lifted by the size of the token's values
+                float top = -INFINITY;
+#pragma unroll 1
+                for (int c0 = 0; c0 < kQwBlock; c0 += 32) {
+                    uint32_t acc[32];
+                    __syncwarp();
+                    tmem_load_issue(tm_s + c0, acc);
+                    tmem_load_wait(acc);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int c = c0 + 16 * h;
+                        if (!masked && !stage.per_token[c >> 4]) {
+                            float m = fmax3(__uint_as_float(acc[16 * h]), __uint_as_float(acc[16 * h + 1]), __uint_as_float(acc[16 * h + 2]));
+#pragma unroll
+                            for (int i = 3; i < 15; i += 2)
+                                m = fmax3(m, __uint_as_float(acc[16 * h + i]), __uint_as_float(acc[16 * h + i + 1]));
+                            m = fmaxf(m, __uint_as_float(acc[16 * h + 15]));
+                            top = fmaxf(top, fmaf(m, factor * stage.k_factor[c], stage.v_exp[c]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (pos + c + i < sees)
+                                    top = fmaxf(top, fmaf(__uint_as_float(acc[16 * h + i]), factor * stage.k_factor[c + i], stage.v_exp[c + i]));
+                        }
+                    }
+                }
+                // ---- move the reference if it is exceeded by much
+                if (b == 0) {
+                    ref = top > -1e37f ? top : 0.f;
+                } else if (__any_sync(0xFFFFFFFFu, top > ref + kQaSlack)) {
+                    const float to = fmaxf(ref, top), f = exp2_fast(ref - to);
+                    ref = to;
+                    l *= f;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < HD; c0 += 32) {
+                        uint32_t acc[32];
+                        tmem_load_issue(tm_o + c0, acc);
+                        tmem_load_wait(acc);
+#pragma unroll
+                        for (int q8 = 0; q8 < 4; ++q8) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(__uint_as_float(acc[8 * q8 + i]) * f);
+                            tmem_store8(tm_o + c0 + 8 * q8, w);
+                        }
+                    }
+                }
+                // ---- weights (times 2^e of the token's values) over the scores that have been read
+#pragma unroll 1
+                for (int c0 = 0; c0 < kQwBlock; c0 += 32) {
+                    uint32_t acc[32];
+                    __syncwarp();
+                    tmem_load_issue(tm_s + c0, acc);
+                    tmem_load_wait(acc);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int c = c0 + 16 * h;
+                        uint32_t w[8];
+                        if (!masked && !stage.per_token[c >> 4]) {
+                            const float f = factor * stage.k_factor[c], e = stage.v_exp[c], shift = e - ref;
+                            float sum = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float x0 = exp2_fast(fmaf(__uint_as_float(acc[16 * h + 2 * i]), f, shift));
+                                const float x1 = exp2_fast(fmaf(__uint_as_float(acc[16 * h + 2 * i + 1]), f, shift));
+                                sum += x0 + x1;
+                                w[i] = pack_half2(x0, x1);
+                            }
+                            l = fmaf(sum, exp2_fast(fminf(-e, 126.f)), l);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                float x[2];
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const int col = c + 2 * i + k;
+                                    const float e = stage.v_exp[col];
+                                    x[k] = exp2_fast(fmaf(__uint_as_float(acc[16 * h + 2 * i + k]), factor * stage.k_factor[col], e - ref));
+                                    if (pos + col >= sees) x[k] = 0.f;
+                                    l = fmaf(x[k], exp2_fast(fminf(-e, 126.f)), l);
+                                }
+                                w[i] = pack_half2(x[0], x[1]);
+                            }
+                        }
+                        __syncwarp();
+                        tmem_store8(tm_s + (uint32_t)(c >> 1), w);
+                    }
+                }
+                tmem_store_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sy.p_ready[t]);
+            }
+            if (!ok) break;
+            // ---- the item's rows, or this block's part of them
+            if (!(ok = wait(&sy.o_done[t], items & 1, kAggTimeoutAcc))) break;
+            ++items;
+            tc_fence_after_sync();
+            const bool whole = it.block == 0 && n_blocks == it.units;
+            float* slot = p.partial + (size_t)(2 * blockIdx.x + (it.block > 0 ? 0 : 1)) * qw_slot_floats(HD);
+            const int grow = row0 + r, token = grow / p.group, h = it.head * p.group + grow - token * p.group;
+            const size_t at = ((size_t)it.seq * p.q_len + token) * p.q_heads + h;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+            for (int c0 = 0; c0 < HD; c0 += 32) {
+                uint32_t acc[32];
+                __syncwarp();
+                tmem_load_issue(tm_o + c0, acc);
+                tmem_load_wait(acc);
+                if (r >= n_rows) {
+                    // a lane without a row only takes part in the loads
+                } else if (whole) {
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            w[i] = Half16<T>::pack(l == 0.f ? 0.f : __uint_as_float(acc[8 * q4 + 2 * i]) * inv,
+                                                   l == 0.f ? 0.f : __uint_as_float(acc[8 * q4 + 2 * i + 1]) * inv);
+                        *reinterpret_cast<uint4*>(p.out + (at * HD + c0 + 8 * q4) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int q4 = 0; q4 < 8; ++q4)
+                        *reinterpret_cast<uint4*>(slot + (size_t)r * HD + c0 + 4 * q4) =
+                            make_uint4(acc[4 * q4], acc[4 * q4 + 1], acc[4 * q4 + 2], acc[4 * q4 + 3]);
+                }
+            }
+            if (r < n_rows) {
+                if (!whole)
+                    *reinterpret_cast<float2*>(slot + (size_t)kQwRows * HD + 2 * r) = make_float2(l == 0.f ? kQaNoMax : ref, l);
+                else if (p.lse)
+                    p.lse[at] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (u < units) qw_next(p, it);
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Joins partial results, writes the rows that see nothing, and makes everything NaN if a wait of the main
+// kernel ran out.  grid (heads * row blocks * 8, n_seq): 32 rows a block, HD / 4 threads a row.
+template <typename T, int HD>
+__global__ void __launch_bounds__(HD / 4 * 8) quant_attention_wide_join_kernel(const __grid_constant__ QuantAttnParams p)
+{
+    wait_for_prior_kernels();
+    const int seq = blockIdx.y, len = qw_len(p, seq), q_len = qw_q_len(p, seq);
+    const int row_blocks = (q_len * p.group + kQwRows - 1) / kQwRows;
+    const int item = blockIdx.x >> 3, part = blockIdx.x & 7;
+    if (row_blocks == 0 || item >= row_blocks * p.n_heads) return;
+    const int head = item / row_blocks, row_block = item - head * row_blocks;
+    const int row0 = row_block * kQwRows, rows = min(kQwRows, q_len * p.group - row0);
+    const int ch = threadIdx.x % (HD / 4) * 4;
+    bool failed = false;
+    for (int b = threadIdx.x & 31; b < p.blocks; b += 32) failed |= p.status[b] != 0;
+    failed = __any_sync(0xFFFFFFFFu, failed);
+    const int units = qw_units(p, len, q_len, row_block);
+    long long first = 0, last = -1, before;
+    if (units > 0) {
+        const long long total = qw_total(p, seq, before), share = qw_share(total, p.blocks);
+        long long unit = before + head * qw_head_units(p, len, q_len);
+        for (int b = 0; b < row_block; ++b) unit += qw_units(p, len, q_len, b);
+        first = unit / share;
+        last = (unit + units - 1) / share;
+        if (first == last && !failed) return;  // written by its block
+    }
+    for (int row = part * 32 + threadIdx.x / (HD / 4); row < min(rows, part * 32 + 32); row += 8) {
+        float m = kQaNoMax, l = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (failed) {
+            l = __int_as_float(0x7FC00000);
+        } else {
+            for (long long b = first; b <= last; ++b) {
+                const float* slot = p.partial + (size_t)(2 * b + (b == first ? 1 : 0)) * qw_slot_floats(HD);
+                const float2 ml = *reinterpret_cast<const float2*>(slot + (size_t)kQwRows * HD + 2 * row);
+                const float4 x = *reinterpret_cast<const float4*>(slot + (size_t)row * HD + ch);
+                const float top = fmaxf(m, ml.x), f0 = exp2_fast(m - top), f1 = exp2_fast(ml.x - top);
+                m = top;
+                l = l * f0 + ml.y * f1;
+                o = make_float4(o.x * f0 + x.x * f1, o.y * f0 + x.y * f1, o.z * f0 + x.z * f1, o.w * f0 + x.w * f1);
+            }
+        }
+        qa_store<T>(p, seq, head, row0 + row, ch, HD, o, m, l);
+    }
+}
+
+}  // namespace civic

@@ -69,7 +69,13 @@ def check(setup, q, out, lse, scale, causal, q_lens=None, canary=None, sample=No
     weighted sum of s * code, which is the output without the minima), elements of P' below 2^-14 of the
     largest to 2^-25 (2^-24 of the largest s * code a token); and the scores' error d, which moves each
     weight by a factor of at most exp(2 d).  A score goes through at most 64 roundings of 2^-23 (32-bit sums
-    that the matrix unit may cut instead of rounding) of partial sums below B = scale * sum |q| (s code + |m|)."""
+    that the matrix unit may cut instead of rounding) of partial sums below B = scale * sum |q| (s code + |m|).
+
+    The kernels for many rows (bf16, heads up to 128) round v to fp16, by half a step of 2^-11, or by 2^-25
+    against 2^-7 of the tile's largest (2^-18 of it), and weights the same way (below 2^-14 of the largest by
+    2^-25).  Their scores are exact products but for K groups whose scale is below 2^-5 of the tile's largest S:
+    such a scale is off by at most 2^-25 against 2^-9 (2^-16 S), a value of up to 16 of them by 2^-12 S."""
+    wide = setup.dtype == torch.bfloat16 and setup.dim <= 128 and q.shape[1] * (q.shape[2] // setup.cache.n_heads) > 16
     read, rows = setup.reader()
     eps = torch.finfo(setup.dtype).eps / 2
     for s, n in enumerate(setup.lens_host):
@@ -100,6 +106,11 @@ def check(setup, q, out, lse, scale, causal, q_lens=None, canary=None, sample=No
             b = float(((kk - km[:seen, h // group] + km[:seen, h // group].abs()) @ x.abs()).max() * abs(scale))
             d = 64 * 2.0**-23 * b + 2.0**-20
             codes = vv - mm
+            if wide:
+                steps = parts["k"][1][:seen, h // group].double().nan_to_num(0.0)
+                if bool((steps < steps.max() * 2.0**-5).any()):
+                    d += 2.0**-12 * float(steps.max() * x.abs().sum()) * abs(scale)
+                codes = vv.abs() + 2.0**-7 * vv.abs().max()
             tol = eps * want.abs() * 1.01 + 2.0**-11 * (w @ codes) + seen * 2.0**-24 * float(w.max()) * codes.amax(0) \
                 + (math.exp(2 * d) - 1) * vv.abs().amax(0) + torch.finfo(setup.dtype).tiny
             off = (o - want).abs()
@@ -142,6 +153,161 @@ def test_against_64_bits(case, causal, spare):
     check(setup, q, out, lse, dim**-0.5, causal, sample=150)
     again, lse2 = attend(setup, q, causal=causal)
     assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+WIDE = [  # lens, heads, q_heads, dim, bits, page, q_len
+    ([1], 1, 32, 128, 4, 16, 1),
+    ([40], 1, 20, 64, 8, 16, 40),
+    ([127, 128, 129, 0, 300], 2, 8, 128, 4, 16, 33),
+    ([500, 20, 61], 2, 14, 64, 4, 48, 61),
+    ([700, 257], 3, 3, 128, 8, 64, 129),
+    ([1000], 2, 8, 128, 4, 32, 300),
+    ([300, 299, 5], 1, 4, 64, 8, 128, 300),
+    ([2500], 1, 5, 128, 8, 16, 52),
+    ([513], 1, 8, 64, 4, 256, 32),
+]
+
+
+@pytest.mark.parametrize("case", WIDE)
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_rows_against_64_bits(case, causal):
+    lens, heads, q_heads, dim, bits, page, q_len = case
+    setup = Setup(lens, heads, dim, bits, page, torch.bfloat16, seed=23)
+    q = setup.queries(q_len, q_heads)
+    out, lse = attend(setup, q, causal=causal)
+    check(setup, q, out, lse, dim**-0.5, causal, sample=200)
+    again, lse2 = attend(setup, q, causal=causal)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    # as a whole no further off than a rounding to bf16 may be, whatever the operands' roundings add up to
+    read, rows = setup.reader()
+    n = lens[0]
+    want, want_lse = oq.attention(q[0, -40:], *(read.rows(0, w, rows[0], n) for w in "kv"), dim**-0.5, causal)
+    assert float((out[0, -40:].double() - want).norm() / want.norm()) < 2.0**-8
+    seen = torch.isfinite(want_lse)
+    assert float((lse[0, -40:].double() - want_lse)[seen].abs().max()) < 2.0**-14
+
+
+def test_many_rows_padded_batch():
+    setup = Setup([400, 130, 100, 0, 31], 2, 128, 4, 16, torch.bfloat16, seed=24)
+    q = setup.queries(70, 8)
+    for q_lens in ([70, 1, 0, 2, 64], [33, 64, 70, 0, 70], [1, 65, 64, 70, -4]):
+        some = torch.tensor(q_lens, dtype=torch.int32, device=DEV)
+        out = torch.full((5, 70, 8, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((5, 70, 8), 7.0, dtype=torch.float32, device=DEV)
+        civic.civic_quant_attention(q.to(DEV), setup.cache, 0, setup.table, setup.lens, q_lens=some, out=out, lse=lse)
+        check(setup, q, out.cpu(), lse.cpu(), 128**-0.5, True, q_lens=[min(max(x, 0), 70) for x in q_lens], canary=7.0, sample=120)
+
+
+def test_many_rows_many_items():
+    rng = np.random.default_rng(25)
+    lens = [int(x) for x in rng.integers(0, 200, 70)]
+    lens[33] = 3000
+    setup = Setup(lens, 2, 64, 4, 16, torch.bfloat16, seed=25)
+    q = setup.queries(9, 6)
+    out, lse = attend(setup, q)
+    check(setup, q, out, lse, 0.125, True, sample=12)
+
+
+def test_many_rows_masked_tokens_may_hold_anything():
+    """NaN rows of later query tokens stay out of the earlier ones' results."""
+    def edit(k, v):
+        k[0, 150:], v[0, 150:] = float("nan"), float("inf")
+        v[0, 145] = float("nan")
+
+    setup = Setup([160], 2, 64, 4, 16, torch.bfloat16, seed=26, edit=edit)
+    q = setup.queries(20, 8)  # tokens 140 .. 159
+
+    def same_rows(k, v):
+        k[0], v[0] = setup.k[0, :145].float(), setup.v[0, :145].float()
+
+    out, lse = attend(setup, q)
+    clean = Setup([145], 2, 64, 4, 16, torch.bfloat16, seed=26, edit=same_rows)
+    check(clean, q[:, :5], out[:, :5], lse[:, :5], 0.125, True)
+    assert bool(torch.isnan(out[:, 5:]).all()) and bool(torch.isnan(lse[:, 10:]).all())
+
+
+def test_many_rows_nan_in_v_stays_in_its_group_where_all_see_it():
+    def edit(k, v):
+        v[0, 20, 1, 40] = float("nan")
+
+    setup = Setup([400], 2, 128, 8, 16, torch.bfloat16, seed=27, edit=edit)
+    out, lse = attend(setup, setup.queries(10, 8))
+    assert bool(torch.isnan(out[0, :, 4:, 32:64]).all()) and bool(torch.isfinite(lse).all())
+    assert int(torch.isnan(out).sum()) == 10 * 4 * 32
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("kind", ["large_scores", "sink", "tiny_v", "huge_v", "tiny_q", "zero_q", "equal_rows", "uneven", "negative"])
+def test_many_rows_extreme_ranges(bits, kind):
+    def edit(k, v):
+        if kind == "sink":
+            k[:, 3] = -4.0
+            v[:, 3] *= 2.0**30
+        elif kind == "tiny_v":
+            v *= 2.0**-70
+        elif kind == "huge_v":
+            v *= 2.0**70
+        elif kind == "equal_rows":
+            k[:], v[:] = 1.25, -3.5
+        elif kind == "uneven":  # tokens of one tile that differ by far more than fp16's range allows
+            size = torch.exp2(torch.randint(-30, 4, k.shape[:2] + (1, 1), generator=torch.Generator().manual_seed(1)).float())
+            k *= size
+            v *= size.flip(1)
+
+    setup = Setup([277, 20], 1, 64, bits, 16, torch.bfloat16, seed=28, edit=edit, k_scale=8.0 if kind == "large_scores" else 1.0)
+    q = setup.queries(12, 3, {"large_scores": 60.0, "tiny_q": 2.0**-110, "zero_q": 0.0}.get(kind, 1.0))
+    if kind == "sink":
+        q = q.abs() * 2
+    scale = {"tiny_q": 2.0**105, "negative": -0.2}.get(kind, 0.125)
+    out, lse = attend(setup, q, scale=scale)
+    check(setup, q, out, lse, scale, True)
+
+
+def test_many_rows_bad_pages_are_left_out():
+    setup = Setup([300], 2, 128, 4, 16, torch.bfloat16, seed=29)
+    q = setup.queries(8, 8)
+    for bad in (-1, setup.cache.n_pages, 2**31 - 1):
+        setup.table[0, 2] = bad
+        record = torch.zeros(4, dtype=torch.int32, device=DEV)
+        with civic.index_check(record):
+            out, lse = attend(setup, q, causal=False)
+        assert record.tolist() == [3, 0, 2, bad]
+        read, rows = setup.reader()
+        keep = [t for t in range(300) if not 32 <= t < 48]
+        k, v = (read.rows(0, w, rows[0], 300)[keep] for w in "kv")
+        want, want_lse = oq.attention(q[0], k, v, 128**-0.5, False)
+        assert float((out[0].double() - want).norm() / want.norm()) < 2.0**-8
+        assert float((lse[0].double() - want_lse).abs().max()) < 2.0**-14
+
+
+def test_many_rows_captured_and_replayed_and_on_two_streams():
+    setup = Setup([600, 290], 2, 128, 4, 16, torch.bfloat16, seed=30)
+    q = setup.queries(30, 8).to(DEV)
+    out = torch.empty_like(q)
+    need = civic.quant_attention_workspace_bytes(setup.cache, setup.table.shape[1], 2, 30, 8)
+    ws = [torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    lens = setup.lens.clone()
+    run = lambda: civic.civic_quant_attention(q, setup.cache, 0, setup.table, lens, out=out, workspace=ws[0])
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for now in ([600, 290], [30, 64], [0, 289], [7, 0]):
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        out.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, _ = civic.civic_quant_attention(q, setup.cache, 0, setup.table, lens, workspace=ws[1])
+        assert torch.equal(out, want)
+    lens.copy_(setup.lens)
+    want, _ = civic.civic_quant_attention(q, setup.cache, 0, setup.table, lens)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [civic.civic_quant_attention(q, setup.cache, 0, setup.table, lens, workspace=ws[1 + i % 2], stream=streams[i % 2])[0]
+           for i in range(12)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in got)
 
 
 @pytest.mark.parametrize("spare", [0, 65])
