@@ -205,6 +205,12 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
+__device__ __forceinline__ uint32_t half2_sub(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) { return Half16<__half>::pack(lo, hi); }
 template <int OFFSET>
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src)
@@ -547,6 +553,18 @@ struct QaWarp {
                         }
                     }
                 }
+                // Codes are not negative: over many tokens their weighted sum and the minima's are both far larger than
+                // what they add up to.  Where the result has 11 bits that loss shows, and codes are taken from the
+                // middle of their range instead: c - 8 (16 times that in odd nibbles) or c - 128, and m + 8 s.
+                float mid[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    mid[r] = kHalf ? fmaf(H::lo(par[r][j]), BITS == 4 ? 8.f : 128.f, H::hi(par[r][j])) : H::hi(par[r][j]);
+                if constexpr (kHalf)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) a[h][k] = half2_sub(a[h][k], BITS == 4 && !(k & 1) ? 0x00080008u : 0x00800080u);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float x[4];
@@ -555,7 +573,7 @@ struct QaWarp {
 #pragma unroll
                         for (int b = 0; b < 2; ++b) {
                             const float w_p = c[nt][2 * r + b];
-                            float scaled = w_p * H::lo(par[r][j]), low = w_p * H::hi(par[r][j]);
+                            float scaled = w_p * H::lo(par[r][j]), low = w_p * mid[r];
                             if (MASK && pos + g + 8 * r >= limit[nt][b]) scaled = low = 0.f;  // whatever the tile holds there
                             x[2 * r + b] = scaled;
                             v_min[nt][b][j] += low;
