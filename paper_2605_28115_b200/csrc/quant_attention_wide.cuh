@@ -3,7 +3,7 @@
 // rows = query tokens x query heads of the K/V head.
 //
 // With many rows the products outweigh the unpacking, so every code is turned into its value once
-// per block of 256 rows: eight warps read tiles, make fp16 numbers of them and lay them into shared
+// per block of 256 rows: seven warps read tiles, make fp16 numbers of them and lay them into shared
 // memory as tcgen05 operands; one warp issues the products; eight warps hold the softmax of two tiles
 // of 128 rows, one row per thread:
 //   producers  K', V' [128 tokens, HD], 128-byte swizzled; queries of the next item
@@ -36,11 +36,13 @@ namespace civic {
 
 constexpr int kQwBlock = 128;      // tokens per unit
 constexpr int kQwRows = 256;       // query rows per item: two tiles of 128
-constexpr int kQwProducers = 8;    // warps that unpack: one tile of 16 tokens each
+constexpr int kQwTiles = kQwBlock / kQuantTile;
+constexpr int kQwProducers = 7;    // warps that unpack tiles in turn; 16 warps in all, so that each may have 128 registers
 constexpr int kQwThreads = 32 * (8 + 1 + kQwProducers);
 constexpr int kQwMaxBlocks = 148;
 constexpr int kQwMinUnits = 2;
 constexpr float kQwDropped = -3e38f;  // exponent of a token that is left out
+constexpr float kQwSlack = 12.f;      // a weight stays below 2^12 times the reference's
 
 struct QwItem {
     int seq, head, row_block, block;   // block: the next unit of the item
@@ -164,7 +166,8 @@ __host__ __device__ constexpr uint32_t qw_idesc(int n, int b_mn_major)
 struct QwStage {                     // beside a V' stage
     float k_factor[kQwBlock];        // 2^e of the token's K'
     float v_exp[kQwBlock];           // e of its V', kQwDropped for a token that is left out
-    int per_token[kQwProducers];     // tile's tokens have factors of their own
+    float v_down[kQwBlock];          // 2^-e, 0 for such a token
+    int per_token[kQwTiles];         // tile's tokens have factors of their own
 };
 struct QwSync {
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full;
@@ -195,6 +198,14 @@ __device__ __forceinline__ uint64_t qw_mid_desc(uint32_t smem_addr)
 constexpr size_t kQwStatusBytes = 1024;
 __host__ __device__ constexpr size_t qw_slot_floats(int hd) { return (size_t)kQwRows * (hd + 2); }
 
+// 8 columns, waited for (with whatever else this warp has asked for)
+__device__ __forceinline__ void tmem_load8(uint32_t taddr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c)
 {
     uint32_t d;
@@ -309,8 +320,8 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
     int* status = p.status + blockIdx.x;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sy.k_full[i], kQwProducers);
-            mbar_init(&sy.v_full[i], kQwProducers);
+            mbar_init(&sy.k_full[i], kQwTiles);
+            mbar_init(&sy.v_full[i], kQwTiles);
             mbar_init(&sy.k_empty[i], 1);
             mbar_init(&sy.v_empty[i], 1);
             mbar_init(&sy.s_full[i], 1);
@@ -342,20 +353,19 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
     };
 
     if (warp >= 9 && units > 0) {
-        // ---- producers: warp pw takes tile pw of each block of 128 tokens
+        // ---- producers: the share's tiles, eight to a block of 128 tokens, in turn
         const int pw = warp - 9, g = lane >> 2, t = lane & 3;
         const int row = (g >> 1) + 4 * (g & 1);  // K rows of a quarter of the warp: 4 apart, so that its stores hit all banks
         const int64_t page_stride = (int64_t)p.n_heads * p.page_tiles * Tile::kBytes;
         uint32_t* kp = sy.params[pw][0];
         uint32_t* vp = sy.params[pw][1];
-        QwItem nx = it;         // the block whose tile is in registers
-        int left = units;       // blocks from it on
-        // one tile's codes, fetched a block ahead
+        QwItem nx = it;         // the block of the tile in registers
+        // one tile's codes, fetched ahead
         uint32_t kw[2][Tile::kWords], vw[2][Tile::kWords], k_par[NG / 2], v_par[NG / 2];
         const char* tile = nullptr;  // NULL: no token of the tile is there
         bool found = true;           // its page exists
-        auto fetch = [&]() {
-            const int n = nx.block * 8 + pw;
+        auto fetch = [&](int i) {
+            const int n = nx.block * kQwTiles + i;
             tile = nullptr;
             found = true;
             if (n * kQuantTile >= nx.len) return;
@@ -392,67 +402,73 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                     }
                 }
         };
-        fetch();
+        fetch(pw);
         bool ok = true;
-        for (int u = 0, seg = 0; ok && u < units; ++seg) {
-            // the item's queries, once the products of the previous item's scores are done
-            if (u > 0 && !(ok = wait(&sy.k_empty[(u - 1) % kKStages], ((u - 1) / kKStages) & 1, kAggTimeoutEmpty))) break;
-            const int n_blocks = min(units - u, it.units - it.block), n_rows = it.q_len * p.group - it.row_block * kQwRows;
-            const int seen_by_all = qw_sees(p, it.len, it.q_len, it.row_block * kQwRows);
+        int seg = -1, seg_end = 0, seen_by_all = 0;  // item number, its first block behind, tokens that all its rows see
+        for (int n = pw; n < units * kQwTiles; n += kQwProducers) {
+            const int u = n / kQwTiles, i = n % kQwTiles;
+            if (u == seg_end) {
+                // the next item's queries, once the products of the previous item's scores are done
+                if (u > 0 && !(ok = wait(&sy.k_empty[(u - 1) % kKStages], ((u - 1) / kKStages) & 1, kAggTimeoutEmpty))) break;
+                if (u > 0) qw_next(p, it);
+                ++seg;
+                seg_end += min(units - u, it.units - it.block);
+                const int n_rows = it.q_len * p.group - it.row_block * kQwRows;
+                seen_by_all = qw_sees(p, it.len, it.q_len, it.row_block * kQwRows);
 #pragma unroll 1
-            for (int pass = 0; pass < 4; ++pass) {
-                const int r = pw * 32 + pass * 8 + g;  // row of the item
-                if (pw >= 4 && n_rows <= 128) break;
-                const int grow = it.row_block * kQwRows + r, token = grow / p.group, sub = grow - token * p.group;
-                float f[NG][8], top = 0.f;
+                for (int r0 = pw * 8; r0 < (n_rows > 128 ? 256 : 128); r0 += kQwProducers * 8) {
+                    const int r = r0 + g;  // row of the item
+                    const int grow = it.row_block * kQwRows + r, token = grow / p.group, sub = grow - token * p.group;
+                    float f[NG][8], top = 0.f;
 #pragma unroll
-                for (int j = 0; j < NG; ++j) {
-                    uint4 x = make_uint4(0, 0, 0, 0);
-                    if (r < n_rows)
-                        x = __ldg(reinterpret_cast<const uint4*>(p.q + it.seq * p.q_seq + token * p.q_token +
-                                                                 (it.head * p.group + sub) * p.q_head + (j * 32 + t * 8) * 2));
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    for (int j = 0; j < NG; ++j) {
+                        uint4 x = make_uint4(0, 0, 0, 0);
+                        if (r < n_rows)
+                            x = __ldg(reinterpret_cast<const uint4*>(p.q + it.seq * p.q_seq + token * p.q_token +
+                                                                     (it.head * p.group + sub) * p.q_head + (j * 32 + t * 8) * 2));
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        f[j][i] = (i & 1) ? Half16<T>::hi(w[i >> 1]) : Half16<T>::lo(w[i >> 1]);
-                        top = fmaxf(top, fabsf(f[j][i]));
+                        for (int i = 0; i < 8; ++i) {
+                            f[j][i] = (i & 1) ? Half16<T>::hi(w[i >> 1]) : Half16<T>::lo(w[i >> 1]);
+                            top = fmaxf(top, fabsf(f[j][i]));
+                        }
                     }
-                }
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-                const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 126);
-                const float up = p.scale_log2e < 0.f ? -pow2(14 - e) : pow2(14 - e);  // factors are not negative then
-                if (t == 0) sy.row_factor[seg & 1][r] = pow2(e - 14) * fabsf(p.scale_log2e);
-                uint8_t* at = q_sm + (r >> 7) * kTileBytes + (r & 127) * 128;
-                float mine = 0.f;  // sum over group t
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+                    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 126);
+                    const float up = p.scale_log2e < 0.f ? -pow2(14 - e) : pow2(14 - e);  // factors are not negative then
+                    if (t == 0) sy.row_factor[seg & 1][r] = pow2(e - 14) * fabsf(p.scale_log2e);
+                    uint8_t* at = q_sm + (r >> 7) * kTileBytes + (r & 127) * 128;
+                    float mine = 0.f;  // sum over group t
 #pragma unroll
-                for (int j = 0; j < NG; ++j) {
-                    float sum = 0.f;
+                    for (int j = 0; j < NG; ++j) {
+                        float sum = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        f[j][i] *= up;
-                        sum += f[j][i];
+                        for (int i = 0; i < 8; ++i) {
+                            f[j][i] *= up;
+                            sum += f[j][i];
+                        }
+                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+                        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+                        if (t == j) mine = sum * 0x1p-8f;
+                        // channels in the order in which the codes come out of a word
+                        const uint4 v = BITS == 4
+                                            ? make_uint4(pack_half2(f[j][0], f[j][4]), pack_half2(f[j][1], f[j][5]),
+                                                         pack_half2(f[j][2], f[j][6]), pack_half2(f[j][3], f[j][7]))
+                                            : make_uint4(pack_half2(f[j][0], f[j][2]), pack_half2(f[j][1], f[j][3]),
+                                                         pack_half2(f[j][4], f[j][6]), pack_half2(f[j][5], f[j][7]));
+                        *reinterpret_cast<uint4*>(at + (j >> 1) * 16384 + (((4 * (j & 1) + t) ^ (r & 7)) << 4)) = v;
                     }
-                    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
-                    sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
-                    if (t == j) mine = sum * 0x1p-8f;
-                    // channels in the order in which the codes come out of a word
-                    const uint4 v = BITS == 4
-                                        ? make_uint4(pack_half2(f[j][0], f[j][4]), pack_half2(f[j][1], f[j][5]),
-                                                     pack_half2(f[j][2], f[j][6]), pack_half2(f[j][3], f[j][7]))
-                                        : make_uint4(pack_half2(f[j][0], f[j][2]), pack_half2(f[j][1], f[j][3]),
-                                                     pack_half2(f[j][4], f[j][6]), pack_half2(f[j][5], f[j][7]));
-                    *reinterpret_cast<uint4*>(at + (j >> 1) * 16384 + (((4 * (j & 1) + t) ^ (r & 7)) << 4)) = v;
+                    const float high = Half16<__half>::lo(pack_half2(mine, 0.f));
+                    const uint32_t both = pack_half2(high, mine - high);
+                    *reinterpret_cast<uint2*>(q_mid + (r >> 7) * kQwMidBytes + qw_mid_at(r & 127, t)) = make_uint2(both, both);
                 }
-                const float high = Half16<__half>::lo(pack_half2(mine, 0.f));
-                const uint32_t both = pack_half2(high, mine - high);
-                *reinterpret_cast<uint2*>(q_mid + (r >> 7) * kQwMidBytes + qw_mid_at(r & 127, t)) = make_uint2(both, both);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sy.q_full);
             }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sy.q_full);
-            for (int b = 0; b < n_blocks; ++b, ++u) {
-                const int st = u & 1, phase = (u >> 1) & 1, pos = (nx.block * 8 + pw) * kQuantTile;
+            {
+                const int st = u & 1, phase = (u >> 1) & 1, pos = (nx.block * kQwTiles + i) * kQuantTile;
                 const int k_st = u % kKStages, k_phase = (u / kKStages) & 1;
                 const bool mixed = (nx.block + 1) * kQwBlock > seen_by_all;  // some row does not see all of the block
                 const bool have = tile != nullptr && pos + (lane >> 1) < nx.len;
@@ -460,7 +476,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 // ---- K'
                 if (!(ok = wait(&sy.k_empty[k_st], k_phase ^ 1, kAggTimeoutEmpty))) break;
                 const int ek = qw_params_k<T, HD, BITS>(k_par, kp,
-                                                        k_mid + k_st * kQwMidBytes, pw * 16, have, per_token_k);
+                                                        k_mid + k_st * kQwMidBytes, i * 16, have, per_token_k);
                 // a NaN of V would reach rows that do not see its token through 0 * NaN: it is sent through the
                 // token's factor instead, which only the rows that see it use
                 const int ev = qw_params_v<T, HD, BITS>(v_par, vp, have, mixed,
@@ -469,7 +485,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 uint8_t* k_at = k_sm + k_st * kTileBytes;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int r = row + 8 * h, line = pw * 16 + r;
+                    const int r = row + 8 * h, line = i * 16 + r;
                     uint8_t* at = k_at + line * 128;
 #pragma unroll
                     for (int j = 0; j < NG; ++j) {
@@ -504,11 +520,12 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 if (!(ok = wait(&sy.v_empty[st], phase ^ 1, kAggTimeoutEmpty))) break;
                 QwStage& stage = sy.stage[st];
                 if ((lane & 1) == 0) {
-                    const int c = pw * 16 + (lane >> 1);
+                    const int c = i * 16 + (lane >> 1);
                     stage.k_factor[c] = nan_v ? __int_as_float(0x7FC00000) : pow2(ek);
                     stage.v_exp[c] = found ? (float)ev : kQwDropped;
+                    stage.v_down[c] = found ? pow2(-ev) : 0.f;
                 }
-                if (lane == 0) stage.per_token[pw] = per_token_k || per_token_v;
+                if (lane == 0) stage.per_token[i] = per_token_k || per_token_v;
                 uint8_t* v_at = v_sm + st * kTileBytes;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -534,7 +551,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                             }
                         }
                         const int chunk = 4 * (j & 1) + (g >> 1), off = (j >> 1) * 16384 + (g & 1) * 8;
-                        const int la = pw * 16 + ra, lb = la + 1;
+                        const int la = i * 16 + ra, lb = la + 1;
                         *reinterpret_cast<uint2*>(v_at + off + la * 128 + ((chunk ^ (ra & 7)) << 4)) =
                             make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
                         *reinterpret_cast<uint2*>(v_at + off + lb * 128 + ((chunk ^ (rb & 7)) << 4)) =
@@ -544,12 +561,11 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sy.v_full[st]);
-                if (--left > 0) {
-                    if (++nx.block >= nx.units) qw_next(p, nx);
-                    fetch();
+                if (n + kQwProducers < units * kQwTiles) {
+                    if ((n + kQwProducers) / kQwTiles != u && ++nx.block >= nx.units) qw_next(p, nx);
+                    fetch((n + kQwProducers) % kQwTiles);
                 }
             }
-            if (ok && u < units) qw_next(p, it);
         }
     } else if (warp == 8 && units > 0) {
         // ---- MMA issue; the whole warp walks the loops in step, one elected lane issues
@@ -643,6 +659,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
             const int sees = r < n_rows ? qw_sees(p, it.len, it.q_len, row0 + r) : it.len;
             const int seen_by_all = uniform(qw_sees(p, it.len, it.q_len, row0));
             float ref = 0.f, l = 0.f, factor = 0.f;
+            bool set = false;  // the reference has been taken from a score
             for (int b = 0; b < n_blocks; ++b, ++u, ++turn) {
                 const int st = u & 1, pos = (it.block + b) * kQwBlock;
                 if (!(ok = wait(&sy.s_full[t], turn & 1, kAggTimeoutAcc))) break;
@@ -650,94 +667,95 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 tc_fence_after_sync();
                 if (b == 0) factor = sy.row_factor[seg & 1][r];
                 const QwStage& stage = sy.stage[st];
-                const bool masked = pos + kQwBlock > seen_by_all;
-                // ---- the row's largest logit, lifted by the size of the token's values
-                float top = -INFINITY;
-#pragma unroll 1
-                for (int c0 = 0; c0 < kQwBlock; c0 += 32) {
-                    uint32_t acc[32];
-                    __syncwarp();
-                    tmem_load_issue(tm_s + c0, acc);
-                    tmem_load_wait(acc);
+                int odd = pos + kQwBlock > seen_by_all;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int c = c0 + 16 * h;
-                        if (!masked && !stage.per_token[c >> 4]) {
-                            float m = fmax3(__uint_as_float(acc[16 * h]), __uint_as_float(acc[16 * h + 1]), __uint_as_float(acc[16 * h + 2]));
+                for (int i = 0; i < kQwTiles; ++i) odd |= stage.per_token[i];
+                odd = uniform(odd);
+                // 16 columns: logits relative to the reference, weights (times 2^e of the token's values) as fp16 over
+                // scores that have been read.  One pass: the reference may be exceeded by kQwSlack; beyond that
+                // the row's results so far, P of this block and O, are scaled down (rare after the first block).
+                auto logits = [&](uint32_t (&acc)[16], int c0) {
+                    float top = -INFINITY;
+                    if (!odd) {
+                        const float f = factor * stage.k_factor[c0], shift = stage.v_exp[c0] - ref;
 #pragma unroll
-                            for (int i = 3; i < 15; i += 2)
-                                m = fmax3(m, __uint_as_float(acc[16 * h + i]), __uint_as_float(acc[16 * h + i + 1]));
-                            m = fmaxf(m, __uint_as_float(acc[16 * h + 15]));
-                            top = fmaxf(top, fmaf(m, factor * stage.k_factor[c], stage.v_exp[c]));
-                        } else {
+                        for (int i = 0; i < 16; i += 2) {
+                            const float x0 = fmaf(__uint_as_float(acc[i]), f, shift), x1 = fmaf(__uint_as_float(acc[i + 1]), f, shift);
+                            top = fmax3(top, x0, x1);
+                            acc[i] = __float_as_uint(x0);
+                            acc[i + 1] = __float_as_uint(x1);
+                        }
+                    } else {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                if (pos + c + i < sees)
-                                    top = fmaxf(top, fmaf(__uint_as_float(acc[16 * h + i]), factor * stage.k_factor[c + i], stage.v_exp[c + i]));
+                        for (int i = 0; i < 16; ++i) {
+                            float x = fmaf(__uint_as_float(acc[i]), factor * stage.k_factor[c0 + i], stage.v_exp[c0 + i] - ref);
+                            if (pos + c0 + i >= sees) x = -INFINITY;
+                            top = fmaxf(top, x);
+                            acc[i] = __float_as_uint(x);
                         }
                     }
-                }
-                // ---- move the reference if it is exceeded by much
-                if (b == 0) {
-                    ref = top > -1e37f ? top : 0.f;
-                } else if (__any_sync(0xFFFFFFFFu, top > ref + kQaSlack)) {
-                    const float to = fmaxf(ref, top), f = exp2_fast(ref - to);
-                    ref = to;
-                    l *= f;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < HD; c0 += 32) {
-                        uint32_t acc[32];
-                        tmem_load_issue(tm_o + c0, acc);
-                        tmem_load_wait(acc);
+                    const bool move = set ? top > kQwSlack : top > -1e37f;
+                    if (__any_sync(0xFFFFFFFFu, move)) {
+                        const float up = move ? top : 0.f, f = set ? exp2_fast(-up) : 1.f;  // nothing to scale before
+                        set |= move;
+                        ref += up;
+                        l *= f;
 #pragma unroll
-                        for (int q8 = 0; q8 < 4; ++q8) {
+                        for (int i = 0; i < 16; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) - up);
+                        const uint32_t f2 = pack_half2(f, f);
+#pragma unroll 1
+                        for (int q = 0; q < c0 / 2; q += 8) {
                             uint32_t w[8];
+                            tmem_load8(tm_s + q, w);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(__uint_as_float(acc[8 * q8 + i]) * f);
-                            tmem_store8(tm_o + c0 + 8 * q8, w);
+                            for (int i = 0; i < 8; ++i) w[i] = hmul2(w[i], f2);
+                            tmem_store8(tm_s + q, w);
                         }
+#pragma unroll 1
+                        for (int q = 0; b > 0 && q < HD; q += 8) {
+                            uint32_t w[8];
+                            tmem_load8(tm_o + q, w);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * f);
+                            tmem_store8(tm_o + q, w);
+                        }
+                        tmem_store_wait();
                     }
-                }
-                // ---- weights (times 2^e of the token's values) over the scores that have been read
+                };
+                auto weights = [&](const uint32_t (&acc)[16], int c0) {
+                    float sum = 0.f, sum1 = 0.f;
+                    uint32_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x0 = exp2_fast(__uint_as_float(acc[2 * i])), x1 = exp2_fast(__uint_as_float(acc[2 * i + 1]));
+                        if (!odd) {
+                            sum += x0;
+                            sum1 += x1;
+                        } else {
+                            sum = fmaf(x0, stage.v_down[c0 + 2 * i], sum);
+                            sum1 = fmaf(x1, stage.v_down[c0 + 2 * i + 1], sum1);
+                        }
+                        w[i] = pack_half2(x0, x1);
+                    }
+                    l = odd ? l + (sum + sum1) : fmaf(sum + sum1, stage.v_down[c0], l);
+                    __syncwarp();
+                    tmem_store8(tm_s + (uint32_t)(c0 >> 1), w);
+                };
+                uint32_t even[16], next[16];
+                tmem_load_issue16(tm_s, even);
 #pragma unroll 1
                 for (int c0 = 0; c0 < kQwBlock; c0 += 32) {
-                    uint32_t acc[32];
+                    // a chunk is asked for when the previous one's exponentials are about to start
+                    tmem_load_wait16(even);
+                    logits(even, c0);
                     __syncwarp();
-                    tmem_load_issue(tm_s + c0, acc);
-                    tmem_load_wait(acc);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int c = c0 + 16 * h;
-                        uint32_t w[8];
-                        if (!masked && !stage.per_token[c >> 4]) {
-                            const float f = factor * stage.k_factor[c], e = stage.v_exp[c], shift = e - ref;
-                            float sum = 0.f;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const float x0 = exp2_fast(fmaf(__uint_as_float(acc[16 * h + 2 * i]), f, shift));
-                                const float x1 = exp2_fast(fmaf(__uint_as_float(acc[16 * h + 2 * i + 1]), f, shift));
-                                sum += x0 + x1;
-                                w[i] = pack_half2(x0, x1);
-                            }
-                            l = fmaf(sum, exp2_fast(fminf(-e, 126.f)), l);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                float x[2];
-#pragma unroll
-                                for (int k = 0; k < 2; ++k) {
-                                    const int col = c + 2 * i + k;
-                                    const float e = stage.v_exp[col];
-                                    x[k] = exp2_fast(fmaf(__uint_as_float(acc[16 * h + 2 * i + k]), factor * stage.k_factor[col], e - ref));
-                                    if (pos + col >= sees) x[k] = 0.f;
-                                    l = fmaf(x[k], exp2_fast(fminf(-e, 126.f)), l);
-                                }
-                                w[i] = pack_half2(x[0], x[1]);
-                            }
-                        }
-                        __syncwarp();
-                        tmem_store8(tm_s + (uint32_t)(c >> 1), w);
-                    }
+                    tmem_load_issue16(tm_s + c0 + 16, next);
+                    weights(even, c0);
+                    tmem_load_wait16(next);
+                    logits(next, c0 + 16);
+                    __syncwarp();
+                    if (c0 + 32 < kQwBlock) tmem_load_issue16(tm_s + c0 + 32, even);
+                    weights(next, c0 + 16);
                 }
                 tmem_store_wait();
                 tc_fence_before_sync();
