@@ -779,7 +779,7 @@ class QuantCache:
     queries and of the outputs."""
 
     __slots__ = ("buffer", "page_size", "head_dim", "bits", "dtype", "n_layers", "n_pages", "n_heads", "device", "desc_ref",
-                 "ptr", "layer_bytes", "_tables")
+                 "ptr", "layer_bytes", "_tables")  # desc_ref: the description as a C argument
 
     def __init__(self, buffer: torch.Tensor, page_size: int, head_dim: int, bits: int, dtype: torch.dtype = torch.bfloat16):
         code = QUANT_DTYPES.get(dtype)
@@ -789,12 +789,12 @@ class QuantCache:
             raise ValueError("buffer must be a CUDA tensor [n_layers, n_pages, n_heads, page bytes]")
         self.ptr = _dev_ptr(buffer, "buffer", torch.uint8)
         self.n_layers, self.n_pages, self.n_heads, per_head = buffer.shape
-        self.desc_ref = ctypes.byref(QuantDesc(self.n_pages, page_size, self.n_heads, head_dim, bits, code))
-        self.layer_bytes = self.n_pages * load().civic_quant_page_bytes(self.desc_ref)
-        if self.layer_bytes == 0:
+        self.desc_ref, page_bytes = _quant_desc(self.n_pages, page_size, self.n_heads, head_dim, bits, code)
+        if page_bytes == 0:
             raise CivicError(5, "QuantCache")
-        if self.layer_bytes != self.n_pages * self.n_heads * per_head:
+        if page_bytes != self.n_heads * per_head:
             raise ValueError("buffer's last dimension must be page_size / 16 * quant_tile_bytes(head_dim, bits)")
+        self.layer_bytes = self.n_pages * page_bytes
         self.buffer, self.page_size, self.head_dim, self.bits, self.dtype = buffer, page_size, head_dim, bits, dtype
         self.device, self._tables = buffer.device, None
 
@@ -806,10 +806,39 @@ class QuantCache:
         return self._tables
 
 
-@functools.lru_cache(maxsize=None)
+# ctypes objects that depend on a few numbers only; making them takes longer than looking them up
+
+
+@functools.lru_cache(maxsize=256)
 def _pointer_array(n: int):
-    """The ctypes type of n pointers (creating one takes microseconds)."""
+    """The type of n pointers."""
     return ctypes.c_void_p * n
+
+
+@functools.lru_cache(maxsize=256)
+def _quant_desc(*fields):
+    """(civic_quant_desc_t as an argument, bytes of a page or 0)"""
+    ref = ctypes.byref(QuantDesc(*fields))
+    return ref, load().civic_quant_page_bytes(ref)
+
+
+@functools.lru_cache(maxsize=256)
+def _row_strides(seq: int, token: int, head: int):
+    """civic_row_strides_t as an argument"""
+    return ctypes.byref(RowStrides(seq, token, head))
+
+
+def _call(cache: "QuantCache", where: str, *args, stream: Optional[torch.cuda.Stream]) -> None:
+    """One C call on the cache's device and on `stream` (default: torch's current one), the last argument."""
+    fn = getattr(load(), where)
+    index = cache.device.index
+    if _current_device() == index:
+        status = fn(*args, _stream_ptr(stream))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _stream_ptr(stream))
+    if status:
+        _check(status, where)
 
 
 def quant_cache(n_layers: int, n_pages: int, n_heads: int, head_dim: int, page_size: int = 16, bits: int = 4,
@@ -827,22 +856,21 @@ def _rows_of(cache: QuantCache, x, what: str):
     (pointer table, (n_seq, rows), strides).  Any strides with a contiguous last dimension, the same for all layers."""
     n = cache.n_layers
     if isinstance(x, torch.Tensor):
-        if x.dim() != 5 or x.shape[0] != n:
+        shape, (step, *strides) = x.shape, x.stride() if x.dim() == 5 else (0, 0)
+        if len(shape) != 5 or shape[0] != n:
             raise ValueError(f"{what} must be [n_layers, n_seq, rows, n_heads, head_dim]")
-        _, n_seq, rows, heads, dim = x.shape
-        step, seq, token, head, last = x.stride()
-        first, base = x, x.data_ptr()
-        table = _pointer_array(n)(*[base + 2 * i * step for i in range(n)])
+        first, base, shape = x, x.data_ptr(), shape[1:]
+        table = _pointer_array(n)(*range(base, base + 2 * n * step, 2 * step)) if n > 1 and step > 0 else _pointer_array(n)(*[base] * n)
     else:
         if len(x) != n or any(t.dim() != 4 for t in x):
             raise ValueError(f"{what} must be one [n_seq, rows, n_heads, head_dim] tensor per layer of the cache")
         first = x[0]
-        if any(t.shape != first.shape or t.stride() != first.stride() or t.dtype != first.dtype or t.device != first.device
-               for t in x):
+        shape, strides = first.shape, first.stride()
+        if any(t.shape != shape or t.stride() != strides or t.dtype != first.dtype or t.device != first.device for t in x):
             raise ValueError(f"all {what} tensors must share shape, strides, dtype and device")
-        n_seq, rows, heads, dim = first.shape
-        seq, token, head, last = first.stride()
         table = _pointer_array(n)(*[t.data_ptr() for t in x])
+    n_seq, rows, heads, dim = shape
+    seq, token, head, last = strides
     if heads != cache.n_heads or dim != cache.head_dim or first.dtype is not cache.dtype or last != 1:
         raise ValueError(f"{what} must have the cache's {cache.n_heads} heads of {cache.head_dim} in {cache.dtype}, "
                          "the last dimension contiguous")
@@ -880,10 +908,8 @@ def civic_compact_kv_quant(k_src, v_src, seq_idx: torch.Tensor, cache: QuantCach
     n_seq, seq_len = shape
     idx = _seq_words(cache, seq_idx, n_seq, "seq_idx", 2)
     table = _seq_words(cache, block_table, n_seq, "block_table", 2)
-    with _on_device(cache.device):
-        _check(load().civic_compact_kv_quant(k, v, ctypes.byref(RowStrides(*strides)), cache.n_layers, n_seq, seq_len,
-                                             seq_idx.shape[1], idx, cache.tables(), cache.desc_ref, table,
-                                             block_table.shape[1], _stream_ptr(stream)), "civic_compact_kv_quant")
+    _call(cache, "civic_compact_kv_quant", k, v, _row_strides(*strides), cache.n_layers, n_seq, seq_len, seq_idx.shape[1], idx,
+          cache.tables(), cache.desc_ref, table, block_table.shape[1], stream=stream)
 
 
 def civic_append_kv_quant(k_new, v_new, start: torch.Tensor, cache: QuantCache, block_table: torch.Tensor,
@@ -899,10 +925,8 @@ def civic_append_kv_quant(k_new, v_new, start: torch.Tensor, cache: QuantCache, 
     at = _seq_words(cache, start, n_seq, "start")
     some = _seq_words(cache, counts, n_seq, "counts")
     table = _seq_words(cache, block_table, n_seq, "block_table", 2)
-    with _on_device(cache.device):
-        _check(load().civic_append_kv_quant(k, v, ctypes.byref(RowStrides(*strides)), cache.n_layers, n_seq, n_new, at, some,
-                                            cache.tables(), cache.desc_ref, table, block_table.shape[1],
-                                            _stream_ptr(stream)), "civic_append_kv_quant")
+    _call(cache, "civic_append_kv_quant", k, v, _row_strides(*strides), cache.n_layers, n_seq, n_new, at, some, cache.tables(),
+          cache.desc_ref, table, block_table.shape[1], stream=stream)
 
 
 def civic_read_kv_quant(cache: QuantCache, block_table: torch.Tensor, counts: torch.Tensor, k_out, v_out,
@@ -918,10 +942,8 @@ def civic_read_kv_quant(cache: QuantCache, block_table: torch.Tensor, counts: to
     some = _seq_words(cache, counts, n_seq, "counts")
     at = _seq_words(cache, start, n_seq, "start")
     table = _seq_words(cache, block_table, n_seq, "block_table", 2)
-    with _on_device(cache.device):
-        _check(load().civic_read_kv_quant(cache.tables(), cache.desc_ref, table, block_table.shape[1], cache.n_layers, n_seq,
-                                          rows, at, some, k, v, ctypes.byref(RowStrides(*strides)), _stream_ptr(stream)),
-               "civic_read_kv_quant")
+    _call(cache, "civic_read_kv_quant", cache.tables(), cache.desc_ref, table, block_table.shape[1], cache.n_layers, n_seq, rows,
+          at, some, k, v, _row_strides(*strides), stream=stream)
     return k_out, v_out
 
 
@@ -939,8 +961,10 @@ def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_
     q [n_seq, q_len, q_heads, head_dim], any strides with a contiguous last dimension; lens int32 [n_seq] tokens in the
     cache, the query tokens among them (causal: they are the last ones); q_lens int32 [n_seq] query tokens of each
     sequence (default: all q_len), rows behind them are left as they were."""
-    n_seq, q_len, q_heads, dim = q.shape if q.dim() == 4 else (0, 0, 0, -1)
-    seq, token, head, last = q.stride() if q.dim() == 4 else (0, 0, 0, -1)
+    if q.dim() != 4:
+        raise ValueError("q must be [n_seq, q_len, q_heads, head_dim]")
+    n_seq, q_len, q_heads, dim = q.shape
+    seq, token, head, last = q.stride()
     if dim != cache.head_dim or q.dtype is not cache.dtype or last != 1:
         raise ValueError(f"q must be [n_seq, q_len, q_heads, {cache.head_dim}] in {cache.dtype}, its last dimension contiguous")
     if not 0 <= layer < cache.n_layers:
@@ -954,7 +978,7 @@ def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_
     max_pages = block_table.shape[1]
     made = []  # allocated here: not to be handed out again before `stream` is done with it
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=dev)
         made.append(out)
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
@@ -975,13 +999,10 @@ def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_
     if stream is not None:
         for t in made:
             t.record_stream(stream)
-    with _on_device(dev):
-        _check(lib.civic_quant_attention(
-            q.data_ptr(), ctypes.byref(RowStrides(seq, token, head)), cache.ptr + layer * cache.layer_bytes, cache.desc_ref,
-            table, max_pages, n_tok, n_q, n_seq, q_len, q_heads, dim ** -0.5 if scale is None else scale, causal,
-            _dev_ptr(out, "out", cache.dtype), _dev_ptr(lse, "lse", torch.float32),
-            _dev_ptr(workspace, "workspace", torch.uint8), 0 if workspace is None else workspace.numel(),
-            _stream_ptr(stream)), "civic_quant_attention")
+    _call(cache, "civic_quant_attention", q.data_ptr(), _row_strides(seq, token, head), cache.ptr + layer * cache.layer_bytes,
+          cache.desc_ref, table, max_pages, n_tok, n_q, n_seq, q_len, q_heads, dim ** -0.5 if scale is None else scale, causal,
+          _dev_ptr(out, "out", cache.dtype), _dev_ptr(lse, "lse", torch.float32), _dev_ptr(workspace, "workspace", torch.uint8),
+          0 if workspace is None else workspace.numel(), stream=stream)
     return out, lse
 
 

@@ -174,7 +174,7 @@ struct QwSync {
     uint64_t s_full[2], p_ready[2], o_done[2], drained;
     float row_factor[2][kQwRows];    // per item (alternating) and row: takes raw scores to base-2 logits
     QwStage stage[2];
-    uint32_t params[kQwProducers][2][kQuantTile * 4];  // per producer warp, K | V: {s, m} as fp16, [token][group]
+    alignas(16) uint32_t params[kQwProducers][2][kQuantTile * 4];  // per producer warp, K | V: {s, m} as fp16, [token][group]
     uint32_t tmem_base;
     int abort;
 };
@@ -198,6 +198,22 @@ __device__ __forceinline__ uint64_t qw_mid_desc(uint32_t smem_addr)
 constexpr size_t kQwStatusBytes = 1024;
 __host__ __device__ constexpr size_t qw_slot_floats(int hd) { return (size_t)kQwRows * (hd + 2); }
 
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
 // 8 columns, waited for (with whatever else this warp has asked for)
 __device__ __forceinline__ void tmem_load8(uint32_t taddr, uint32_t (&r)[8])
 {
@@ -221,6 +237,20 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
 // Floor of log2, within -100 .. 119 (larger numbers overflow fp16 and end as NaN).
 __device__ __forceinline__ int qw_log2(float x) { return min(max((int)(__float_as_uint(x) >> 23) - 127, -100), 119); }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+
+// N 32-bit words from shared memory aligned to them (N = 2 or 4)
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint32_t* at)
+{
+    if constexpr (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        w[0] = v.x;
+        w[1] = v.y;
+    } else {
+        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    }
+}
 
 // Both functions prepare one tile's scales and minima for the fp16 arithmetic, by a warp: lane = (token
 // lane / 2, every second group from lane % 2 on).  They return the exponent of the lane's token.
@@ -360,49 +390,59 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
         uint32_t* kp = sy.params[pw][0];
         uint32_t* vp = sy.params[pw][1];
         QwItem nx = it;         // the block of the tile in registers
-        // one tile's codes, fetched ahead
+        // one tile's codes, K and V fetched ahead separately: each as soon as its registers are free
         uint32_t kw[2][Tile::kWords], vw[2][Tile::kWords], k_par[NG / 2], v_par[NG / 2];
-        const char* tile = nullptr;  // NULL: no token of the tile is there
+        const char* tile = nullptr;  // NULL: no token of the tile is there (its codes are zeros then)
         bool found = true;           // its page exists
-        auto fetch = [&](int i) {
+        int page = -1;
+        auto look_up = [&](int i) {  // the page of tile i of block nx
             const int n = nx.block * kQwTiles + i;
-            tile = nullptr;
-            found = true;
-            if (n * kQuantTile >= nx.len) return;
-            const int slot = p.page_magic ? (int)__umulhi((uint32_t)n, p.page_magic) : n;
-            const int page = __ldg(p.block_table + (size_t)nx.seq * p.max_pages + slot);
-            if ((uint32_t)page >= (uint32_t)p.n_pages) {
-                found = false;
-                if (p.check && lane == 0) report_bad_index(p.check, kIndexBadPage, nx.seq, slot, page);
-                return;
-            }
-            tile = p.cache + page * page_stride + ((int64_t)nx.head * p.page_tiles + (n - slot * p.page_tiles)) * Tile::kBytes;
-            const uint32_t* kc = reinterpret_cast<const uint32_t*>(tile);
-            const uint32_t* vc = reinterpret_cast<const uint32_t*>(tile + Tile::kVCodes);
+            page = -1;
+            if (n * kQuantTile < nx.len)
+                page = __ldg(p.block_table + (size_t)nx.seq * p.max_pages + (p.page_magic ? (int)__umulhi((uint32_t)n, p.page_magic) : n));
+        };
+        auto load_params = [&]() {
+            if (!tile) return;
 #pragma unroll
             for (int i = 0; i < NG / 2; ++i) {
                 const int at = (lane >> 1) * NG + (lane & 1) + 2 * i;
                 k_par[i] = __ldg(reinterpret_cast<const uint32_t*>(tile + Tile::kKParams) + at);
                 v_par[i] = __ldg(reinterpret_cast<const uint32_t*>(tile + Tile::kVParams) + at);
             }
+        };
+        auto load = [&](uint32_t (&w)[2][Tile::kWords], bool v) {
+            const uint32_t* codes = reinterpret_cast<const uint32_t*>(tile + (v ? Tile::kVCodes : 0));
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int pl = 0; pl < Tile::kPlanes; ++pl) {
-                    const uint32_t* ka = kc + Tile::k_word(row + 8 * h, t, pl * Tile::kPlane);
-                    const uint32_t* va = vc + Tile::v_word(h, lane, pl * Tile::kPlane);
+                    const uint32_t* at = codes + (v ? Tile::v_word(h, lane, pl * Tile::kPlane) : Tile::k_word(row + 8 * h, t, pl * Tile::kPlane));
                     if constexpr (Tile::kPlane == 4) {
-                        const uint4 a = __ldg(reinterpret_cast<const uint4*>(ka)), b = __ldg(reinterpret_cast<const uint4*>(va));
-                        kw[h][4 * pl] = a.x; kw[h][4 * pl + 1] = a.y; kw[h][4 * pl + 2] = a.z; kw[h][4 * pl + 3] = a.w;
-                        vw[h][4 * pl] = b.x; vw[h][4 * pl + 1] = b.y; vw[h][4 * pl + 2] = b.z; vw[h][4 * pl + 3] = b.w;
+                        const uint4 a = tile ? __ldg(reinterpret_cast<const uint4*>(at)) : make_uint4(0, 0, 0, 0);
+                        w[h][4 * pl] = a.x; w[h][4 * pl + 1] = a.y; w[h][4 * pl + 2] = a.z; w[h][4 * pl + 3] = a.w;
                     } else {
-                        const uint2 a = __ldg(reinterpret_cast<const uint2*>(ka)), b = __ldg(reinterpret_cast<const uint2*>(va));
-                        kw[h][0] = a.x; kw[h][1] = a.y;
-                        vw[h][0] = b.x; vw[h][1] = b.y;
+                        const uint2 a = tile ? __ldg(reinterpret_cast<const uint2*>(at)) : make_uint2(0, 0);
+                        w[h][0] = a.x; w[h][1] = a.y;
                     }
                 }
         };
-        fetch(pw);
+        auto locate = [&](int i) {  // the tile whose page has been looked up
+            const int n = nx.block * kQwTiles + i, slot = p.page_magic ? (int)__umulhi((uint32_t)n, p.page_magic) : n;
+            tile = nullptr;
+            found = true;
+            if (n * kQuantTile >= nx.len) return;
+            if ((uint32_t)page < (uint32_t)p.n_pages) {
+                tile = p.cache + page * page_stride + ((int64_t)nx.head * p.page_tiles + (n - slot * p.page_tiles)) * Tile::kBytes;
+            } else {
+                found = false;
+                if (p.check && lane == 0) report_bad_index(p.check, kIndexBadPage, nx.seq, slot, page);
+            }
+        };
+        look_up(pw);
+        locate(pw);
+        load_params();
+        load(kw, false);
+        load(vw, true);
         bool ok = true;
         int seg = -1, seg_end = 0, seen_by_all = 0;  // item number, its first block behind, tokens that all its rows see
         for (int n = pw; n < units * kQwTiles; n += kQwProducers) {
@@ -487,28 +527,25 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 for (int h = 0; h < 2; ++h) {
                     const int r = row + 8 * h, line = i * 16 + r;
                     uint8_t* at = k_at + line * 128;
+                    uint32_t pars[NG];
+                    load_words(pars, kp + r * NG);
 #pragma unroll
                     for (int j = 0; j < NG; ++j) {
-                        const uint32_t par = kp[r * NG + j];
+                        const uint32_t par = pars[j];
                         const uint32_t s = __byte_perm(par, par, 0x1010), n8 = __byte_perm(par, par, 0x3232);
                         uint8_t* to = at + (j >> 1) * 16384 + (((4 * (j & 1) + t) ^ (r & 7)) << 4);
-                        uint4 v = make_uint4(0, 0, 0, 0);
+                        uint4 v;
                         if constexpr (BITS == 4) {
-                            if (tile) {
-                                const uint32_t x = kw[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);  // s / 16
-                                v = make_uint4(hfma2(x & 0x000F000Fu, s, n8), hfma2(x & 0x00F000F0u, s16, n8),
-                                               hfma2(y & 0x000F000Fu, s, n8), hfma2(y & 0x00F000F0u, s16, n8));
-                            }
+                            const uint32_t x = kw[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);  // s / 16
+                            v = make_uint4(hfma2(x & 0x000F000Fu, s, n8), hfma2(x & 0x00F000F0u, s16, n8),
+                                           hfma2(y & 0x000F000Fu, s, n8), hfma2(y & 0x00F000F0u, s16, n8));
                         } else {
-                            uint4 high = make_uint4(0, 0, 0, 0);
-                            if (tile) {
-                                const uint32_t x = kw[h][2 * j], y = kw[h][2 * j + 1], n128 = hmul2(n8, 0x4C004C00u);  // times 16
-                                v = make_uint4(hfma2(x & 0x000F000Fu, s, n8), hfma2((x >> 8) & 0x000F000Fu, s, n8),
-                                               hfma2(y & 0x000F000Fu, s, n8), hfma2((y >> 8) & 0x000F000Fu, s, n8));
-                                high = make_uint4(hfma2(x & 0x00F000F0u, s, n128), hfma2((x >> 8) & 0x00F000F0u, s, n128),
-                                                  hfma2(y & 0x00F000F0u, s, n128), hfma2((y >> 8) & 0x00F000F0u, s, n128));
-                            }
-                            *reinterpret_cast<uint4*>(to + kTileBytes) = high;
+                            const uint32_t x = kw[h][2 * j], y = kw[h][2 * j + 1], n128 = hmul2(n8, 0x4C004C00u);  // times 16
+                            v = make_uint4(hfma2(x & 0x000F000Fu, s, n8), hfma2((x >> 8) & 0x000F000Fu, s, n8),
+                                           hfma2(y & 0x000F000Fu, s, n8), hfma2((y >> 8) & 0x000F000Fu, s, n8));
+                            *reinterpret_cast<uint4*>(to + kTileBytes) =
+                                make_uint4(hfma2(x & 0x00F000F0u, s, n128), hfma2((x >> 8) & 0x00F000F0u, s, n128),
+                                           hfma2(y & 0x00F000F0u, s, n128), hfma2((y >> 8) & 0x00F000F0u, s, n128));
                         }
                         *reinterpret_cast<uint4*>(to) = v;
                     }
@@ -516,39 +553,52 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sy.k_full[k_st]);
+                const bool here = found;
+                const int after = n + kQwProducers, after_i = after % kQwTiles;
+                const bool more = after < units * kQwTiles;
+                if (more) {
+                    if (after / kQwTiles != u && ++nx.block >= nx.units) qw_next(p, nx);
+                    look_up(after_i);
+                }
                 // ---- V' and the tokens' factors
                 if (!(ok = wait(&sy.v_empty[st], phase ^ 1, kAggTimeoutEmpty))) break;
+                if (more) {
+                    locate(after_i);
+                    load_params();
+                    load(kw, false);
+                }
                 QwStage& stage = sy.stage[st];
                 if ((lane & 1) == 0) {
                     const int c = i * 16 + (lane >> 1);
                     stage.k_factor[c] = nan_v ? __int_as_float(0x7FC00000) : pow2(ek);
-                    stage.v_exp[c] = found ? (float)ev : kQwDropped;
-                    stage.v_down[c] = found ? pow2(-ev) : 0.f;
+                    stage.v_exp[c] = here ? (float)ev : kQwDropped;
+                    stage.v_down[c] = here ? pow2(-ev) : 0.f;
                 }
                 if (lane == 0) stage.per_token[i] = per_token_k || per_token_v;
                 uint8_t* v_at = v_sm + st * kTileBytes;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int ra = 8 * h + 2 * t, rb = ra + 1;
+                    uint32_t pars_a[NG], pars_b[NG];
+                    load_words(pars_a, vp + ra * NG);
+                    load_words(pars_b, vp + rb * NG);
 #pragma unroll
                     for (int j = 0; j < NG; ++j) {
-                        const uint32_t pa = vp[ra * NG + j], pb = vp[rb * NG + j];
+                        const uint32_t pa = pars_a[j], pb = pars_b[j];
                         const uint32_t s = __byte_perm(pa, pb, 0x5410), m = __byte_perm(pa, pb, 0x7632);
-                        uint32_t c[4] = {0u, 0u, 0u, 0u};  // channel n of both tokens
-                        if (tile) {
-                            if constexpr (BITS == 4) {
-                                const uint32_t x = vw[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);
-                                c[0] = hfma2(x & 0x000F000Fu, s, m);
-                                c[1] = hfma2(x & 0x00F000F0u, s16, m);
-                                c[2] = hfma2(y & 0x000F000Fu, s, m);
-                                c[3] = hfma2(y & 0x00F000F0u, s16, m);
-                            } else {
-                                const uint32_t x = vw[h][2 * j], y = vw[h][2 * j + 1];
-                                c[0] = hfma2(x & 0x00FF00FFu, s, m);
-                                c[1] = hfma2((x >> 8) & 0x00FF00FFu, s, m);
-                                c[2] = hfma2(y & 0x00FF00FFu, s, m);
-                                c[3] = hfma2((y >> 8) & 0x00FF00FFu, s, m);
-                            }
+                        uint32_t c[4];  // channel n of both tokens
+                        if constexpr (BITS == 4) {
+                            const uint32_t x = vw[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);
+                            c[0] = hfma2(x & 0x000F000Fu, s, m);
+                            c[1] = hfma2(x & 0x00F000F0u, s16, m);
+                            c[2] = hfma2(y & 0x000F000Fu, s, m);
+                            c[3] = hfma2(y & 0x00F000F0u, s16, m);
+                        } else {
+                            const uint32_t x = vw[h][2 * j], y = vw[h][2 * j + 1];
+                            c[0] = hfma2(x & 0x00FF00FFu, s, m);
+                            c[1] = hfma2((x >> 8) & 0x00FF00FFu, s, m);
+                            c[2] = hfma2(y & 0x00FF00FFu, s, m);
+                            c[3] = hfma2((y >> 8) & 0x00FF00FFu, s, m);
                         }
                         const int chunk = 4 * (j & 1) + (g >> 1), off = (j >> 1) * 16384 + (g & 1) * 8;
                         const int la = i * 16 + ra, lb = la + 1;
@@ -561,10 +611,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sy.v_full[st]);
-                if (n + kQwProducers < units * kQwTiles) {
-                    if ((n + kQwProducers) / kQwTiles != u && ++nx.block >= nx.units) qw_next(p, nx);
-                    fetch((n + kQwProducers) % kQwTiles);
-                }
+                if (more) load(vw, true);
             }
         }
     } else if (warp == 8 && units > 0) {
@@ -671,23 +718,35 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
 #pragma unroll
                 for (int i = 0; i < kQwTiles; ++i) odd |= stage.per_token[i];
                 odd = uniform(odd);
-                // 16 columns: logits relative to the reference, weights (times 2^e of the token's values) as fp16 over
+                // 32 columns: logits relative to the reference, weights (times 2^e of the token's values) as fp16 over
                 // scores that have been read.  One pass: the reference may be exceeded by kQwSlack; beyond that
                 // the row's results so far, P of this block and O, are scaled down (rare after the first block).
-                auto logits = [&](uint32_t (&acc)[16], int c0) {
+                auto logits = [&](uint32_t (&acc)[32], int c0) {
                     float top = -INFINITY;
                     if (!odd) {
-                        const float f = factor * stage.k_factor[c0], shift = stage.v_exp[c0] - ref;
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            const float x0 = fmaf(__uint_as_float(acc[i]), f, shift), x1 = fmaf(__uint_as_float(acc[i + 1]), f, shift);
-                            top = fmax3(top, x0, x1);
-                            acc[i] = __float_as_uint(x0);
-                            acc[i + 1] = __float_as_uint(x1);
+                        for (int h = 0; h < 2; ++h) {
+                            const float f = factor * stage.k_factor[c0 + 16 * h], shift = stage.v_exp[c0 + 16 * h] - ref;
+#pragma unroll
+                            for (int i = 16 * h; i < 16 * h + 16; i += 2) {
+                                const float2 x = fma2(make_float2(__uint_as_float(acc[i]), __uint_as_float(acc[i + 1])), make_float2(f, f),
+                                                      make_float2(shift, shift));
+                                acc[i] = __float_as_uint(x.x);
+                                acc[i + 1] = __float_as_uint(x.y);
+                            }
                         }
+                        float m[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            m[q] = fmax3(__uint_as_float(acc[8 * q]), __uint_as_float(acc[8 * q + 1]), __uint_as_float(acc[8 * q + 2]));
+                            m[q] = fmax3(m[q], __uint_as_float(acc[8 * q + 3]), __uint_as_float(acc[8 * q + 4]));
+                            m[q] = fmax3(m[q], __uint_as_float(acc[8 * q + 5]), __uint_as_float(acc[8 * q + 6]));
+                            m[q] = fmaxf(m[q], __uint_as_float(acc[8 * q + 7]));
+                        }
+                        top = fmaxf(fmax3(m[0], m[1], m[2]), m[3]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
+                        for (int i = 0; i < 32; ++i) {
                             float x = fmaf(__uint_as_float(acc[i]), factor * stage.k_factor[c0 + i], stage.v_exp[c0 + i] - ref);
                             if (pos + c0 + i >= sees) x = -INFINITY;
                             top = fmaxf(top, x);
@@ -701,7 +760,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                         ref += up;
                         l *= f;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) - up);
+                        for (int i = 0; i < 32; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) - up);
                         const uint32_t f2 = pack_half2(f, f);
 #pragma unroll 1
                         for (int q = 0; q < c0 / 2; q += 8) {
@@ -722,40 +781,37 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                         tmem_store_wait();
                     }
                 };
-                auto weights = [&](const uint32_t (&acc)[16], int c0) {
-                    float sum = 0.f, sum1 = 0.f;
-                    uint32_t w[8];
+                // `half_way` is called when the first 16 scores are done with: their registers may take the next ones
+                auto weights = [&](const uint32_t (&acc)[32], int c0, auto half_way) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float x0 = exp2_fast(__uint_as_float(acc[2 * i])), x1 = exp2_fast(__uint_as_float(acc[2 * i + 1]));
-                        if (!odd) {
-                            sum += x0;
-                            sum1 += x1;
-                        } else {
-                            sum = fmaf(x0, stage.v_down[c0 + 2 * i], sum);
-                            sum1 = fmaf(x1, stage.v_down[c0 + 2 * i + 1], sum1);
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1) half_way();
+                        float2 sum = make_float2(0.f, 0.f);
+                        uint32_t w[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            const int i = 16 * h + 2 * q;
+                            const float2 x = make_float2(exp2_fast(__uint_as_float(acc[i])), exp2_fast(__uint_as_float(acc[i + 1])));
+                            sum = odd ? fma2(x, make_float2(stage.v_down[c0 + i], stage.v_down[c0 + i + 1]), sum) : add2(x, sum);
+                            w[q] = pack_half2(x.x, x.y);
                         }
-                        w[i] = pack_half2(x0, x1);
+                        l = odd ? l + (sum.x + sum.y) : fmaf(sum.x + sum.y, stage.v_down[c0 + 16 * h], l);
+                        __syncwarp();
+                        tmem_store8(tm_s + (uint32_t)(c0 >> 1) + 8u * h, w);
                     }
-                    l = odd ? l + (sum + sum1) : fmaf(sum + sum1, stage.v_down[c0], l);
-                    __syncwarp();
-                    tmem_store8(tm_s + (uint32_t)(c0 >> 1), w);
                 };
-                uint32_t even[16], next[16];
-                tmem_load_issue16(tm_s, even);
+                uint32_t even[32], next[32];
+                tmem_load_issue(tm_s, even);
 #pragma unroll 1
-                for (int c0 = 0; c0 < kQwBlock; c0 += 32) {
-                    // a chunk is asked for when the previous one's exponentials are about to start
-                    tmem_load_wait16(even);
+                for (int c0 = 0; c0 < kQwBlock; c0 += 64) {
+                    tmem_load_wait(even);
                     logits(even, c0);
-                    __syncwarp();
-                    tmem_load_issue16(tm_s + c0 + 16, next);
-                    weights(even, c0);
-                    tmem_load_wait16(next);
-                    logits(next, c0 + 16);
-                    __syncwarp();
-                    if (c0 + 32 < kQwBlock) tmem_load_issue16(tm_s + c0 + 32, even);
-                    weights(next, c0 + 16);
+                    weights(even, c0, [&]() { tmem_load_issue(tm_s + c0 + 32, next); });
+                    tmem_load_wait(next);
+                    logits(next, c0 + 32);
+                    weights(next, c0 + 32, [&]() {
+                        if (c0 + 64 < kQwBlock) tmem_load_issue(tm_s + c0 + 64, even);
+                    });
                 }
                 tmem_store_wait();
                 tc_fence_before_sync();
