@@ -207,14 +207,16 @@ civic_status_t move_impl(const MoveCall& c, void* stream_)
     return CIVIC_OK;
 }
 
-// Column tiles of 8 query rows that a warp of the attention kernel takes at once: enough for all
-// rows of a K/V head, as far as registers hold the accumulators (HD / 16 * 4 for each).
-int attention_tiles(int head_dim, int64_t rows)
+// Column tiles of 8 query rows that a warp of the attention kernel takes at once: all rows of a K/V head
+// as far as registers hold the accumulators (HD / 16 * 4 for each), else equal parts of them.  Unpacking is
+// done once per pass (48 sequences, 35 rows, heads of 64 in 8 bits: 88 us in one pass of five tiles, 91 us in
+// two of three, 107 us in two of four).  bf16 rows beyond 16 never come here but for heads of 256 (wide_rows).
+int attention_tiles(const civic_quant_desc_t& d, int64_t rows)
 {
-    const int most = head_dim == 64 ? 4 : (head_dim == 128 ? 2 : 1);
-    int nt = 1;
-    while (nt < most && rows > 8 * nt) nt *= 2;
-    return nt;
+    const int64_t most = d.head_dim == 64 ? (d.dtype == CIVIC_FP16 ? 5 : 2) : (d.head_dim == 128 ? 2 : 1);
+    const int64_t passes = (rows + 8 * most - 1) / (8 * most);
+    const int64_t nt = passes == 0 ? 1 : (rows + 8 * passes - 1) / (8 * passes);
+    return nt == 4 ? 5 : (int)nt;
 }
 
 template <typename T, int HD, int BITS, int NT>
@@ -290,10 +292,14 @@ template <typename T>
 civic_status_t launch_attention_dim(const civic_quant_desc_t& d, int nt, civic::QuantAttnParams& p, unsigned items,
                                     cudaStream_t stream)
 {
-    if (d.head_dim == 64)
-        return nt == 1 ? launch_attention_bits<T, 64, 1>(d.bits, p, items, stream)
-                       : (nt == 2 ? launch_attention_bits<T, 64, 2>(d.bits, p, items, stream)
-                                  : launch_attention_bits<T, 64, 4>(d.bits, p, items, stream));
+    if (d.head_dim == 64) {
+        if (nt == 1) return launch_attention_bits<T, 64, 1>(d.bits, p, items, stream);
+        if constexpr (std::is_same<T, __half>::value) {
+            if (nt == 3) return launch_attention_bits<T, 64, 3>(d.bits, p, items, stream);
+            if (nt == 5) return launch_attention_bits<T, 64, 5>(d.bits, p, items, stream);
+        }
+        return launch_attention_bits<T, 64, 2>(d.bits, p, items, stream);
+    }
     if (d.head_dim == 128)
         return nt == 1 ? launch_attention_bits<T, 128, 1>(d.bits, p, items, stream)
                        : launch_attention_bits<T, 128, 2>(d.bits, p, items, stream);
@@ -328,7 +334,7 @@ size_t attention_workspace(const civic_quant_desc_t& d, int32_t max_pages, int32
     if (wide_rows(d, q_len, q_heads))
         return civic::kQwStatusBytes + (size_t)2 * civic::kQwMaxBlocks * civic::qw_slot_floats(d.head_dim) * 4;
     if (whole_items(d, max_pages)) return 0;
-    const int nt = attention_tiles(d.head_dim, (int64_t)q_len * (q_heads / d.n_heads));
+    const int nt = attention_tiles(d, (int64_t)q_len * (q_heads / d.n_heads));
     return round_up((size_t)2 * civic::kQaMaxBlocks * 8 * nt * (d.head_dim + 2) * 4, 256);
 }
 
@@ -447,7 +453,7 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     p.check = g_index_check;
     p.blocks = whole_items(d, max_pages_per_seq) ? 0 : 1;  // 1: sized to the device below
     const int64_t rows = (int64_t)q_len * p.group;
-    const int nt = attention_tiles(d.head_dim, rows);
+    const int nt = attention_tiles(d, rows);
     const unsigned items = (unsigned)((rows + 8 * nt - 1) / (8 * nt) * d.n_heads);
     // a block's share of the tiles, of at least 148 blocks', is counted in 32 bits
     if ((double)n_seq * items * (p.capacity / civic::kQuantTile) > 148.0 * (1 << 30)) return CIVIC_ERR_UNSUPPORTED;

@@ -721,9 +721,9 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 // 32 columns: logits relative to the reference, weights (times 2^e of the token's values) as fp16 over
                 // scores that have been read.  One pass: the reference may be exceeded by kQwSlack; beyond that
                 // the row's results so far, P of this block and O, are scaled down (rare after the first block).
-                auto logits = [&](uint32_t (&acc)[32], int c0) {
+                auto logits = [&](auto per_column, uint32_t (&acc)[32], int c0) {
                     float top = -INFINITY;
-                    if (!odd) {
+                    if constexpr (!decltype(per_column)::value) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const float f = factor * stage.k_factor[c0 + 16 * h], shift = stage.v_exp[c0 + 16 * h] - ref;
@@ -782,7 +782,8 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                     }
                 };
                 // `half_way` is called when the first 16 scores are done with: their registers may take the next ones
-                auto weights = [&](const uint32_t (&acc)[32], int c0, auto half_way) {
+                auto weights = [&](auto per_column, const uint32_t (&acc)[32], int c0, auto half_way) {
+                    constexpr bool kPerColumn = decltype(per_column)::value;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (h == 1) half_way();
@@ -792,27 +793,32 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                         for (int q = 0; q < 8; ++q) {
                             const int i = 16 * h + 2 * q;
                             const float2 x = make_float2(exp2_fast(__uint_as_float(acc[i])), exp2_fast(__uint_as_float(acc[i + 1])));
-                            sum = odd ? fma2(x, make_float2(stage.v_down[c0 + i], stage.v_down[c0 + i + 1]), sum) : add2(x, sum);
+                            if constexpr (kPerColumn) sum = fma2(x, make_float2(stage.v_down[c0 + i], stage.v_down[c0 + i + 1]), sum);
+                            else sum = add2(x, sum);
                             w[q] = pack_half2(x.x, x.y);
                         }
-                        l = odd ? l + (sum.x + sum.y) : fmaf(sum.x + sum.y, stage.v_down[c0 + 16 * h], l);
+                        l = kPerColumn ? l + (sum.x + sum.y) : fmaf(sum.x + sum.y, stage.v_down[c0 + 16 * h], l);
                         __syncwarp();
                         tmem_store8(tm_s + (uint32_t)(c0 >> 1) + 8u * h, w);
                     }
                 };
-                uint32_t even[32], next[32];
-                tmem_load_issue(tm_s, even);
+                auto block = [&](auto per_column) {
+                    uint32_t even[32], next[32];
+                    tmem_load_issue(tm_s, even);
 #pragma unroll 1
-                for (int c0 = 0; c0 < kQwBlock; c0 += 64) {
-                    tmem_load_wait(even);
-                    logits(even, c0);
-                    weights(even, c0, [&]() { tmem_load_issue(tm_s + c0 + 32, next); });
-                    tmem_load_wait(next);
-                    logits(next, c0 + 32);
-                    weights(next, c0 + 32, [&]() {
-                        if (c0 + 64 < kQwBlock) tmem_load_issue(tm_s + c0 + 64, even);
-                    });
-                }
+                    for (int c0 = 0; c0 < kQwBlock; c0 += 64) {
+                        tmem_load_wait(even);
+                        logits(per_column, even, c0);
+                        weights(per_column, even, c0, [&]() { tmem_load_issue(tm_s + c0 + 32, next); });
+                        tmem_load_wait(next);
+                        logits(per_column, next, c0 + 32);
+                        weights(per_column, next, c0 + 32, [&]() {
+                            if (c0 + 64 < kQwBlock) tmem_load_issue(tm_s + c0 + 64, even);
+                        });
+                    }
+                };
+                if (odd) block(std::true_type{});
+                else block(std::false_type{});
                 tmem_store_wait();
                 tc_fence_before_sync();
                 __syncwarp();
@@ -885,26 +891,39 @@ __global__ void __launch_bounds__(HD / 4 * 8) quant_attention_wide_join_kernel(c
     const int head = item / row_blocks, row_block = item - head * row_blocks;
     const int row0 = row_block * kQwRows, rows = min(kQwRows, q_len * p.group - row0);
     const int ch = threadIdx.x % (HD / 4) * 4;
-    bool failed = false;
-    for (int b = threadIdx.x & 31; b < p.blocks; b += 32) failed |= p.status[b] != 0;
-    failed = __any_sync(0xFFFFFFFFu, failed);
-    const int units = qw_units(p, len, q_len, row_block);
-    long long first = 0, last = -1, before;
-    if (units > 0) {
-        const long long total = qw_total(p, seq, before), share = qw_share(total, p.blocks);
-        long long unit = before + head * qw_head_units(p, len, q_len);
-        for (int b = 0; b < row_block; ++b) unit += qw_units(p, len, q_len, b);
-        first = unit / share;
-        last = (unit + units - 1) / share;
-        if (first == last && !failed) return;  // written by its block
+    // one warp finds out which blocks shared the item
+    __shared__ int shared_first, shared_last, shared_failed;
+    if (threadIdx.x < 32) {
+        bool bad = false;
+        for (int b = threadIdx.x; b < p.blocks; b += 32) bad |= p.status[b] != 0;
+        bad = __any_sync(0xFFFFFFFFu, bad);
+        const int units = qw_units(p, len, q_len, row_block);
+        int first = 0, last = -1;
+        if (units > 0) {
+            long long before;
+            const long long total = qw_total(p, seq, before), share = qw_share(total, p.blocks);
+            long long unit = before + head * qw_head_units(p, len, q_len);
+            for (int b = 0; b < row_block; ++b) unit += qw_units(p, len, q_len, b);
+            first = (int)(unit / share);
+            last = (int)((unit + units - 1) / share);
+        }
+        if (threadIdx.x == 0) {
+            shared_first = first;
+            shared_last = last;
+            shared_failed = bad;
+        }
     }
+    __syncthreads();
+    const int first = shared_first, last = shared_last;
+    const bool failed = shared_failed != 0;
+    if (first == last && !failed) return;  // written by its block
     for (int row = part * 32 + threadIdx.x / (HD / 4); row < min(rows, part * 32 + 32); row += 8) {
         float m = kQaNoMax, l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         if (failed) {
             l = __int_as_float(0x7FC00000);
         } else {
-            for (long long b = first; b <= last; ++b) {
+            for (int b = first; b <= last; ++b) {
                 const float* slot = p.partial + (size_t)(2 * b + (b == first ? 1 : 0)) * qw_slot_floats(HD);
                 const float2 ml = *reinterpret_cast<const float2*>(slot + (size_t)kQwRows * HD + 2 * row);
                 const float4 x = *reinterpret_cast<const float4*>(slot + (size_t)row * HD + ch);
