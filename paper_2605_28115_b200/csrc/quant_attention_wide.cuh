@@ -165,19 +165,23 @@ __host__ __device__ constexpr uint32_t qw_idesc(int n, int b_mn_major)
     return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
 
-struct QwStage {                     // beside a V' stage
-    float k_factor[kQwBlock];        // 2^e of the token's K'
-    float v_exp[kQwBlock];           // e of its V', kQwDropped for a token that is left out
-    float v_down[kQwBlock];          // 2^-e, 0 for such a token
+struct QwKStage {                    // of a block's K'; four of them, since K' may be three blocks ahead of the softmax
+    float factor[kQwBlock];          // 2^e of the token's K'
     int per_token[kQwTiles];         // tile's tokens have factors of their own
+};
+struct QwVStage {                    // beside a V' stage
+    float exp[kQwBlock];             // e of the token's V', kQwDropped for a token that is left out
+    float down[kQwBlock];            // 2^-e, 0 for such a token
+    int per_token[kQwTiles];
 };
 struct QwSync {
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full;
     uint64_t s_full[2][2], p_ready[2][2];  // [tile of rows][half of the block]
     uint64_t pv_done[2], drained;          // products with V issued so far are complete
     float row_factor[2][kQwRows];    // per item (alternating) and row: takes raw scores to base-2 logits
-    QwStage stage[2];
-    alignas(16) uint32_t params[kQwProducers][2][kQuantTile * 4];  // per producer warp, K | V: {s, m} as fp16, [token][group]
+    QwKStage k_stage[4];
+    QwVStage v_stage[2];
+    alignas(16) uint32_t params[kQwProducers][kQuantTile * 4];  // per producer warp: {s, m} as fp16, [token][group]
     uint32_t tmem_base;
     int abort;
 };
@@ -260,7 +264,7 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint32_t* at)
 
 // V: {s 2^24, m} 2^-e.  With clear_nan a NaN group becomes zeros (and `nan` tells the lane's token).
 template <typename T, int HD, int BITS>
-__device__ __forceinline__ int qw_params_v(const uint32_t (&from)[HD / 64], uint32_t* to, bool have, bool clear_nan, bool& per_token, bool& nan)
+__device__ __forceinline__ int qw_params_v(const uint32_t (&from)[HD / 64], uint32_t* to, int rows, bool clear_nan, bool& per_token, bool& nan)
 {
     using H = Half16<T>;
     constexpr int NG = HD / 32;
@@ -269,7 +273,7 @@ __device__ __forceinline__ int qw_params_v(const uint32_t (&from)[HD / 64], uint
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < NG / 2; ++i) {
-        const uint32_t w = have ? from[i] : 0u;
+        const uint32_t w = token < rows ? from[i] : 0u;
         s[i] = H::lo(w);
         m[i] = H::hi(w);
         bad |= m[i] != m[i];
@@ -295,7 +299,7 @@ __device__ __forceinline__ int qw_params_v(const uint32_t (&from)[HD / 64], uint
 // K: {s 2^24, -8 s} 2^-e, and the middles m + 8 s (m + 136 s) 2^(8 - e) as two fp16, each twice, into row
 // `line` of `mid`.
 template <typename T, int HD, int BITS>
-__device__ __forceinline__ int qw_params_k(const uint32_t (&from)[HD / 64], uint32_t* to, uint8_t* mid, int line0, bool have,
+__device__ __forceinline__ int qw_params_k(const uint32_t (&from)[HD / 64], uint32_t* to, uint8_t* mid, int line0, int rows,
                                            bool& per_token)
 {
     using H = Half16<T>;
@@ -304,7 +308,7 @@ __device__ __forceinline__ int qw_params_k(const uint32_t (&from)[HD / 64], uint
     float s[NG / 2], m[NG / 2], s_max = 0.f, mag = 0.f;
 #pragma unroll
     for (int i = 0; i < NG / 2; ++i) {
-        const uint32_t w = have ? from[i] : 0u;
+        const uint32_t w = token < rows ? from[i] : 0u;
         s[i] = H::lo(w);
         m[i] = fmaf(s[i], BITS == 4 ? 8.f : 136.f, H::hi(w));
         s_max = fmaxf(s_max, s[i]);
@@ -389,70 +393,79 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
     };
 
     if (warp >= 9 && units > 0) {
-        // ---- producers: the share's tiles, eight to a block of 128 tokens, in turn
+        // ---- producers: jobs in turn, for each block of 128 tokens eight tiles of K, then eight of V
+        constexpr int kJobs = 2 * kQwTiles;
         const int pw = warp - 9, g = lane >> 2, t = lane & 3;
         const int row = (g >> 1) + 4 * (g & 1);  // K rows of a quarter of the warp: 4 apart, so that its stores hit all banks
         const int64_t page_stride = (int64_t)p.n_heads * p.page_tiles * Tile::kBytes;
-        uint32_t* kp = sy.params[pw][0];
-        uint32_t* vp = sy.params[pw][1];
-        QwItem nx = it;         // the block of the tile in registers
-        // one tile's codes, K and V fetched ahead separately: each as soon as its registers are free
-        uint32_t kw[2][Tile::kWords], vw[2][Tile::kWords], k_par[NG / 2], v_par[NG / 2];
-        const char* tile = nullptr;  // NULL: no token of the tile is there (its codes are zeros then)
-        bool found = true;           // its page exists
-        int page = -1;
-        auto look_up = [&](int i) {  // the page of tile i of block nx
-            const int n = nx.block * kQwTiles + i;
+        uint32_t* params = sy.params[pw];
+        // Three jobs are under way: this one; the next, whose codes are being fetched; and the one after it, whose
+        // page is being looked up.
+        struct Job {
+            int rows;     // tokens of the tile that are there
+            bool found;   // its page exists
+            bool mixed;   // some row of the item does not see all of the block
+        };
+        QwItem nx = it;   // block of the last one
+        int nx_seen = qw_sees(p, nx.len, nx.q_len, nx.row_block * kQwRows);
+        int page = -1, in_page = 0, slot = 0;  // its page, and its tile's place there
+        Job far = {0, true, false}, next = {0, true, false};
+        uint32_t codes[2][Tile::kWords], par[NG / 2];  // of the next job
+        auto look_up = [&](int job) {
+            const int n = nx.block * kQwTiles + (job & (kQwTiles - 1));
+            far.rows = min(max(nx.len - n * kQuantTile, 0), kQuantTile);
+            far.mixed = (nx.block + 1) * kQwBlock > nx_seen;
             page = -1;
-            if (n * kQuantTile < nx.len)
-                page = __ldg(p.block_table + (size_t)nx.seq * p.max_pages + (p.page_magic ? (int)__umulhi((uint32_t)n, p.page_magic) : n));
+            if (far.rows == 0) return;
+            slot = p.page_magic ? (int)__umulhi((uint32_t)n, p.page_magic) : n;
+            in_page = (nx.head * p.page_tiles + (n - slot * p.page_tiles)) * Tile::kBytes;
+            page = __ldg(p.block_table + (size_t)nx.seq * p.max_pages + slot);
         };
-        auto load_params = [&]() {
-            if (!tile) return;
-#pragma unroll
-            for (int i = 0; i < NG / 2; ++i) {
-                const int at = (lane >> 1) * NG + (lane & 1) + 2 * i;
-                k_par[i] = __ldg(reinterpret_cast<const uint32_t*>(tile + Tile::kKParams) + at);
-                v_par[i] = __ldg(reinterpret_cast<const uint32_t*>(tile + Tile::kVParams) + at);
+        auto fetch = [&](int job) {
+            next = far;
+            next.found = far.rows == 0 || (uint32_t)page < (uint32_t)p.n_pages;
+            if (!next.found) {
+                next.rows = 0;
+                if (p.check && lane == 0) report_bad_index(p.check, kIndexBadPage, nx.seq, slot, page);
             }
-        };
-        auto load = [&](uint32_t (&w)[2][Tile::kWords], bool v) {
-            const uint32_t* codes = reinterpret_cast<const uint32_t*>(tile + (v ? Tile::kVCodes : 0));
+            const bool v = (job & kQwTiles) != 0, there = next.rows > 0;
+            const char* tile = p.cache + page * page_stride + in_page;
+            const uint32_t* from = reinterpret_cast<const uint32_t*>(tile + (v ? Tile::kVCodes : 0));
+#pragma unroll
+            for (int i = 0; i < NG / 2; ++i)
+                par[i] = there ? __ldg(reinterpret_cast<const uint32_t*>(tile + (v ? Tile::kVParams : Tile::kKParams)) +
+                                       (lane >> 1) * NG + (lane & 1) + 2 * i)
+                               : 0u;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int pl = 0; pl < Tile::kPlanes; ++pl) {
-                    const uint32_t* at = codes + (v ? Tile::v_word(h, lane, pl * Tile::kPlane) : Tile::k_word(row + 8 * h, t, pl * Tile::kPlane));
+                    const uint32_t* at = from + (v ? Tile::v_word(h, lane, pl * Tile::kPlane) : Tile::k_word(row + 8 * h, t, pl * Tile::kPlane));
                     if constexpr (Tile::kPlane == 4) {
-                        const uint4 a = tile ? __ldg(reinterpret_cast<const uint4*>(at)) : make_uint4(0, 0, 0, 0);
-                        w[h][4 * pl] = a.x; w[h][4 * pl + 1] = a.y; w[h][4 * pl + 2] = a.z; w[h][4 * pl + 3] = a.w;
+                        const uint4 a = there ? __ldg(reinterpret_cast<const uint4*>(at)) : make_uint4(0, 0, 0, 0);
+                        codes[h][4 * pl] = a.x; codes[h][4 * pl + 1] = a.y; codes[h][4 * pl + 2] = a.z; codes[h][4 * pl + 3] = a.w;
                     } else {
-                        const uint2 a = tile ? __ldg(reinterpret_cast<const uint2*>(at)) : make_uint2(0, 0);
-                        w[h][0] = a.x; w[h][1] = a.y;
+                        const uint2 a = there ? __ldg(reinterpret_cast<const uint2*>(at)) : make_uint2(0, 0);
+                        codes[h][0] = a.x; codes[h][1] = a.y;
                     }
                 }
         };
-        auto locate = [&](int i) {  // the tile whose page has been looked up
-            const int n = nx.block * kQwTiles + i, slot = p.page_magic ? (int)__umulhi((uint32_t)n, p.page_magic) : n;
-            tile = nullptr;
-            found = true;
-            if (n * kQuantTile >= nx.len) return;
-            if ((uint32_t)page < (uint32_t)p.n_pages) {
-                tile = p.cache + page * page_stride + ((int64_t)nx.head * p.page_tiles + (n - slot * p.page_tiles)) * Tile::kBytes;
-            } else {
-                found = false;
-                if (p.check && lane == 0) report_bad_index(p.check, kIndexBadPage, nx.seq, slot, page);
-            }
-        };
+        const int n_jobs = units * kJobs;
         look_up(pw);
-        locate(pw);
-        load_params();
-        load(kw, false);
-        load(vw, true);
+        fetch(pw);
+        auto advance = [&](int job) {  // to the block of `job`, from that of the job before it in this warp's row
+            if (job / kJobs == (job - kQwProducers) / kJobs || ++nx.block < nx.units) return;
+            qw_next(p, nx);
+            nx_seen = qw_sees(p, nx.len, nx.q_len, nx.row_block * kQwRows);
+        };
+        if (pw + kQwProducers < n_jobs) {
+            advance(pw + kQwProducers);
+            look_up(pw + kQwProducers);
+        }
         bool ok = true;
-        int seg = -1, seg_end = 0, seen_by_all = 0;  // item number, its first block behind, tokens that all its rows see
-        for (int n = pw; n < units * kQwTiles; n += kQwProducers) {
-            const int u = n / kQwTiles, i = n % kQwTiles;
+        int seg = -1, seg_end = 0;  // item number, the first block behind it
+        for (int n = pw; n < n_jobs; n += kQwProducers) {
+            const int u = n / kJobs, i = n & (kQwTiles - 1);
             if (u == seg_end) {
                 // the next item's queries, once the products of the previous item's scores are done
                 if (u > 0 && !(ok = wait(&sy.k_empty[(u - 1) % kKStages], ((u - 1) / kKStages) & 1, kAggTimeoutEmpty))) break;
@@ -460,7 +473,6 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 ++seg;
                 seg_end += min(units - u, it.units - it.block);
                 const int n_rows = it.q_len * p.group - it.row_block * kQwRows;
-                seen_by_all = qw_sees(p, it.len, it.q_len, it.row_block * kQwRows);
 #pragma unroll 1
                 for (int r0 = pw * 8; r0 < (n_rows > 128 ? 256 : 128); r0 += kQwProducers * 8) {
                     const int r = r0 + g;  // row of the item
@@ -513,40 +525,48 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sy.q_full);
             }
-            {
-                const int st = u & 1, phase = (u >> 1) & 1, pos = (nx.block * kQwTiles + i) * kQuantTile;
-                const int k_st = u % kKStages, k_phase = (u / kKStages) & 1;
-                const bool mixed = (nx.block + 1) * kQwBlock > seen_by_all;  // some row does not see all of the block
-                const bool have = tile != nullptr && pos + (lane >> 1) < nx.len;
-                bool per_token_k, per_token_v, nan_v;
+            // this job's codes; the next one's are asked for before the work on them
+            uint32_t w[2][Tile::kWords], pr[NG / 2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < Tile::kWords; ++k) w[h][k] = codes[h][k];
+#pragma unroll
+            for (int k = 0; k < NG / 2; ++k) pr[k] = par[k];
+            const Job job = next;
+            if (n + kQwProducers < n_jobs) {
+                fetch(n + kQwProducers);
+                if (n + 2 * kQwProducers < n_jobs) {
+                    advance(n + 2 * kQwProducers);
+                    look_up(n + 2 * kQwProducers);
+                }
+            }
+            if ((n & kQwTiles) == 0) {
                 // ---- K'
-                if (!(ok = wait(&sy.k_empty[k_st], k_phase ^ 1, kAggTimeoutEmpty))) break;
-                const int ek = qw_params_k<T, HD, BITS>(k_par, kp,
-                                                        k_mid + k_st * kQwMidBytes, i * 16, have, per_token_k);
-                // a NaN of V would reach rows that do not see its token through 0 * NaN: it is sent through the
-                // token's factor instead, which only the rows that see it use
-                const int ev = qw_params_v<T, HD, BITS>(v_par, vp, have, mixed,
-                                                        per_token_v, nan_v);
+                const int k_st = u % kKStages;
+                bool per_token;
+                if (!(ok = wait(&sy.k_empty[k_st], ((u / kKStages) & 1) ^ 1, kAggTimeoutEmpty))) break;
+                const int e = qw_params_k<T, HD, BITS>(pr, params, k_mid + k_st * kQwMidBytes, i * 16, job.rows, per_token);
+                QwKStage& stage = sy.k_stage[u & 3];
+                if ((lane & 1) == 0) stage.factor[i * 16 + (lane >> 1)] = pow2(e);
+                if (lane == 0) stage.per_token[i] = per_token;
                 __syncwarp();
-                uint8_t* k_at = k_sm + k_st * kTileBytes;
+                uint8_t* k_at = k_sm + k_st * kTileBytes + (i * 16 + row) * 128;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int r = row + 8 * h, line = i * 16 + r;
-                    uint8_t* at = k_at + line * 128;
                     uint32_t pars[NG];
-                    load_words(pars, kp + r * NG);
+                    load_words(pars, params + (row + 8 * h) * NG);
 #pragma unroll
                     for (int j = 0; j < NG; ++j) {
-                        const uint32_t par = pars[j];
-                        const uint32_t s = __byte_perm(par, par, 0x1010), n8 = __byte_perm(par, par, 0x3232);
-                        uint8_t* to = at + (j >> 1) * 16384 + (((4 * (j & 1) + t) ^ (r & 7)) << 4);
+                        const uint32_t s = __byte_perm(pars[j], pars[j], 0x1010), n8 = __byte_perm(pars[j], pars[j], 0x3232);
+                        uint8_t* to = k_at + h * 1024 + (j >> 1) * 16384 + (((4 * (j & 1) + t) ^ (row & 7)) << 4);
                         uint4 v;
                         if constexpr (BITS == 4) {
-                            const uint32_t x = kw[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);  // s / 16
+                            const uint32_t x = w[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);  // s / 16
                             v = make_uint4(hfma2(x & 0x000F000Fu, s, n8), hfma2(x & 0x00F000F0u, s16, n8),
                                            hfma2(y & 0x000F000Fu, s, n8), hfma2(y & 0x00F000F0u, s16, n8));
                         } else {
-                            const uint32_t x = kw[h][2 * j], y = kw[h][2 * j + 1], n128 = hmul2(n8, 0x4C004C00u);  // times 16
+                            const uint32_t x = w[h][2 * j], y = w[h][2 * j + 1], n128 = hmul2(n8, 0x4C004C00u);  // times 16
                             v = make_uint4(hfma2(x & 0x000F000Fu, s, n8), hfma2((x >> 8) & 0x000F000Fu, s, n8),
                                            hfma2(y & 0x000F000Fu, s, n8), hfma2((y >> 8) & 0x000F000Fu, s, n8));
                             *reinterpret_cast<uint4*>(to + kTileBytes) =
@@ -559,65 +579,56 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sy.k_full[k_st]);
-                const bool here = found;
-                const int after = n + kQwProducers, after_i = after % kQwTiles;
-                const bool more = after < units * kQwTiles;
-                if (more) {
-                    if (after / kQwTiles != u && ++nx.block >= nx.units) qw_next(p, nx);
-                    look_up(after_i);
-                }
-                // ---- V' and the tokens' factors
-                if (!(ok = wait(&sy.v_empty[st], phase ^ 1, kAggTimeoutEmpty))) break;
-                if (more) {
-                    locate(after_i);
-                    load_params();
-                    load(kw, false);
-                }
-                QwStage& stage = sy.stage[st];
+            } else {
+                // ---- V'
+                const int st = u & 1;
+                bool per_token, nan;
+                if (!(ok = wait(&sy.v_empty[st], ((u >> 1) & 1) ^ 1, kAggTimeoutEmpty))) break;
+                // a NaN of V would reach rows that do not see its token through 0 * NaN: it is sent through the
+                // token's exponent instead, which only the rows that see it use
+                const int e = qw_params_v<T, HD, BITS>(pr, params, job.rows, job.mixed, per_token, nan);
+                QwVStage& stage = sy.v_stage[st];
                 if ((lane & 1) == 0) {
                     const int c = i * 16 + (lane >> 1);
-                    stage.k_factor[c] = nan_v ? __int_as_float(0x7FC00000) : pow2(ek);
-                    stage.v_exp[c] = here ? (float)ev : kQwDropped;
-                    stage.v_down[c] = here ? pow2(-ev) : 0.f;
+                    stage.exp[c] = !job.found ? kQwDropped : (nan ? __int_as_float(0x7FC00000) : (float)e);
+                    stage.down[c] = job.found ? pow2(-e) : 0.f;
                 }
-                if (lane == 0) stage.per_token[i] = per_token_k || per_token_v;
-                uint8_t* v_at = v_sm + st * kTileBytes;
+                if (lane == 0) stage.per_token[i] = per_token;
+                __syncwarp();
+                uint8_t* v_at = v_sm + st * kTileBytes + i * 2048;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int ra = 8 * h + 2 * t, rb = ra + 1;
                     uint32_t pars_a[NG], pars_b[NG];
-                    load_words(pars_a, vp + ra * NG);
-                    load_words(pars_b, vp + rb * NG);
+                    load_words(pars_a, params + ra * NG);
+                    load_words(pars_b, params + rb * NG);
 #pragma unroll
                     for (int j = 0; j < NG; ++j) {
-                        const uint32_t pa = pars_a[j], pb = pars_b[j];
-                        const uint32_t s = __byte_perm(pa, pb, 0x5410), m = __byte_perm(pa, pb, 0x7632);
+                        const uint32_t s = __byte_perm(pars_a[j], pars_b[j], 0x5410), m = __byte_perm(pars_a[j], pars_b[j], 0x7632);
                         uint32_t c[4];  // channel n of both tokens
                         if constexpr (BITS == 4) {
-                            const uint32_t x = vw[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);
+                            const uint32_t x = w[h][j], y = x >> 8, s16 = hmul2(s, 0x2C002C00u);
                             c[0] = hfma2(x & 0x000F000Fu, s, m);
                             c[1] = hfma2(x & 0x00F000F0u, s16, m);
                             c[2] = hfma2(y & 0x000F000Fu, s, m);
                             c[3] = hfma2(y & 0x00F000F0u, s16, m);
                         } else {
-                            const uint32_t x = vw[h][2 * j], y = vw[h][2 * j + 1];
+                            const uint32_t x = w[h][2 * j], y = w[h][2 * j + 1];
                             c[0] = hfma2(x & 0x00FF00FFu, s, m);
                             c[1] = hfma2((x >> 8) & 0x00FF00FFu, s, m);
                             c[2] = hfma2(y & 0x00FF00FFu, s, m);
                             c[3] = hfma2((y >> 8) & 0x00FF00FFu, s, m);
                         }
                         const int chunk = 4 * (j & 1) + (g >> 1), off = (j >> 1) * 16384 + (g & 1) * 8;
-                        const int la = i * 16 + ra, lb = la + 1;
-                        *reinterpret_cast<uint2*>(v_at + off + la * 128 + ((chunk ^ (ra & 7)) << 4)) =
+                        *reinterpret_cast<uint2*>(v_at + off + ra * 128 + ((chunk ^ (ra & 7)) << 4)) =
                             make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
-                        *reinterpret_cast<uint2*>(v_at + off + lb * 128 + ((chunk ^ (rb & 7)) << 4)) =
+                        *reinterpret_cast<uint2*>(v_at + off + rb * 128 + ((chunk ^ (rb & 7)) << 4)) =
                             make_uint2(__byte_perm(c[0], c[1], 0x7632), __byte_perm(c[2], c[3], 0x7632));
                     }
                 }
                 fence_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sy.v_full[st]);
-                if (more) load(vw, true);
             }
         }
     } else if (warp == 8 && units > 0) {
@@ -722,10 +733,11 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                 if (!(ok = wait(&sy.v_full[st], (u >> 1) & 1, kAggTimeoutFull))) break;  // for the factors
                 tc_fence_after_sync();
                 if (b == 0) factor = sy.row_factor[seg & 1][r];
-                const QwStage& stage = sy.stage[st];
+                const QwKStage& ks = sy.k_stage[u & 3];
+                const QwVStage& vs = sy.v_stage[st];
                 int odd = pos + kQwBlock > seen_by_all;
 #pragma unroll
-                for (int i = 0; i < kQwTiles; ++i) odd |= stage.per_token[i];
+                for (int i = 0; i < kQwTiles; ++i) odd |= ks.per_token[i] | vs.per_token[i];
                 odd = uniform(odd);
                 // 32 columns: logits relative to the reference, weights (times 2^e of the token's values) as fp16 over
                 // scores that have been read.  One pass: the reference may be exceeded by kQwSlack; beyond that
@@ -735,7 +747,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                     if constexpr (!decltype(per_column)::value) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const float f = factor * stage.k_factor[c0 + 16 * h], shift = stage.v_exp[c0 + 16 * h] - ref;
+                            const float f = factor * ks.factor[c0 + 16 * h], shift = vs.exp[c0 + 16 * h] - ref;
 #pragma unroll
                             for (int i = 16 * h; i < 16 * h + 16; i += 2) {
                                 const float2 x = fma2(make_float2(__uint_as_float(acc[i]), __uint_as_float(acc[i + 1])), make_float2(f, f),
@@ -756,7 +768,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                     } else {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            float x = fmaf(__uint_as_float(acc[i]), factor * stage.k_factor[c0 + i], stage.v_exp[c0 + i] - ref);
+                            float x = fmaf(__uint_as_float(acc[i]), factor * ks.factor[c0 + i], vs.exp[c0 + i] - ref);
                             if (pos + c0 + i >= sees) x = -INFINITY;
                             top = fmaxf(top, x);
                             acc[i] = __float_as_uint(x);
@@ -807,11 +819,11 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                         for (int q = 0; q < 8; ++q) {
                             const int i = 16 * h + 2 * q;
                             const float2 x = make_float2(exp2_fast(__uint_as_float(acc[i])), exp2_fast(__uint_as_float(acc[i + 1])));
-                            if constexpr (kPerColumn) sum = fma2(x, make_float2(stage.v_down[c0 + i], stage.v_down[c0 + i + 1]), sum);
+                            if constexpr (kPerColumn) sum = fma2(x, make_float2(vs.down[c0 + i], vs.down[c0 + i + 1]), sum);
                             else sum = add2(x, sum);
                             w[q] = pack_half2(x.x, x.y);
                         }
-                        l = kPerColumn ? l + (sum.x + sum.y) : fmaf(sum.x + sum.y, stage.v_down[c0 + 16 * h], l);
+                        l = kPerColumn ? l + (sum.x + sum.y) : fmaf(sum.x + sum.y, vs.down[c0 + 16 * h], l);
                         __syncwarp();
                         tmem_store8(tm_s + (uint32_t)((c0 & 64) + ((c0 & 63) >> 1)) + 8u * h, w);
                     }
