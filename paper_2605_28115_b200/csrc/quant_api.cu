@@ -81,7 +81,11 @@ bool lists_overlap(const void* const* a, int na, size_t a_bytes, const void* con
     return false;
 }
 
-constexpr int64_t kWideRows = 16;
+// The tcgen05 kernels pay once rows are many: below about 40 rows of a K/V head their 128-row tiles are
+// mostly empty, and below about 2048 rows in all too few blocks have work (measured, us, mma.sync / tcgen05:
+// 16 sequences of 4000, 8 heads of 128, 4 bits: 32 rows 69 / 90, 48 rows 97 / 92, 64 rows 123 / 94, 128 rows
+// 233 / 101;  8 of 1000: 32 rows 14 / 27, 64 rows 26 / 28, 128 rows 50 / 30;  1 of 8000: 128 rows 45 / 55).
+constexpr int64_t kWideRows = 40, kWideTotalRows = 2048;
 
 struct MoveCall {
     const void* const* k;  // wide tensors
@@ -210,10 +214,10 @@ civic_status_t move_impl(const MoveCall& c, void* stream_)
 // Column tiles of 8 query rows that a warp of the attention kernel takes at once: all rows of a K/V head
 // as far as registers hold the accumulators (HD / 16 * 4 for each), else equal parts of them.  Unpacking is
 // done once per pass (48 sequences, 35 rows, heads of 64 in 8 bits: 88 us in one pass of five tiles, 91 us in
-// two of three, 107 us in two of four).  bf16 rows beyond 16 never come here but for heads of 256 (wide_rows).
+// two of three, 107 us in two of four).
 int attention_tiles(const civic_quant_desc_t& d, int64_t rows)
 {
-    const int64_t most = d.head_dim == 64 ? (d.dtype == CIVIC_FP16 ? 5 : 2) : (d.head_dim == 128 ? 2 : 1);
+    const int64_t most = d.head_dim == 64 ? 5 : (d.head_dim == 128 ? 2 : 1);
     const int64_t passes = (rows + 8 * most - 1) / (8 * most);
     const int64_t nt = passes == 0 ? 1 : (rows + 8 * passes - 1) / (8 * passes);
     return nt == 4 ? 5 : (int)nt;
@@ -294,11 +298,9 @@ civic_status_t launch_attention_dim(const civic_quant_desc_t& d, int nt, civic::
 {
     if (d.head_dim == 64) {
         if (nt == 1) return launch_attention_bits<T, 64, 1>(d.bits, p, items, stream);
-        if constexpr (std::is_same<T, __half>::value) {
-            if (nt == 3) return launch_attention_bits<T, 64, 3>(d.bits, p, items, stream);
-            if (nt == 5) return launch_attention_bits<T, 64, 5>(d.bits, p, items, stream);
-        }
-        return launch_attention_bits<T, 64, 2>(d.bits, p, items, stream);
+        if (nt == 2) return launch_attention_bits<T, 64, 2>(d.bits, p, items, stream);
+        if (nt == 3) return launch_attention_bits<T, 64, 3>(d.bits, p, items, stream);
+        return launch_attention_bits<T, 64, 5>(d.bits, p, items, stream);
     }
     if (d.head_dim == 128)
         return nt == 1 ? launch_attention_bits<T, 128, 1>(d.bits, p, items, stream)
@@ -318,9 +320,10 @@ civic_status_t check_attention(const civic_quant_desc_t* desc, int32_t n_seq, in
 
 // Whether the call takes the tcgen05 kernels: bf16 only (the other kernels lose less where results have 11
 // bits), heads whose accumulators for 256 rows fit into tensor memory, and enough query rows.
-bool wide_rows(const civic_quant_desc_t& d, int32_t q_len, int32_t q_heads)
+bool wide_rows(const civic_quant_desc_t& d, int32_t n_seq, int32_t q_len, int32_t q_heads)
 {
-    return d.dtype == CIVIC_BF16 && d.head_dim <= 128 && (int64_t)q_len * (q_heads / d.n_heads) > kWideRows;
+    return d.dtype == CIVIC_BF16 && d.head_dim <= 128 && (int64_t)q_len * (q_heads / d.n_heads) > kWideRows &&
+           (int64_t)n_seq * q_len * q_heads > kWideTotalRows;
 }
 
 // Whether an item's tiles are few enough for one block.
@@ -329,9 +332,9 @@ bool whole_items(const civic_quant_desc_t& d, int32_t max_pages)
     return (int64_t)max_pages * d.page_size <= civic::kQaWholeTiles * civic::kQuantTile;
 }
 
-size_t attention_workspace(const civic_quant_desc_t& d, int32_t max_pages, int32_t q_len, int32_t q_heads)
+size_t attention_workspace(const civic_quant_desc_t& d, int32_t max_pages, int32_t n_seq, int32_t q_len, int32_t q_heads)
 {
-    if (wide_rows(d, q_len, q_heads))
+    if (wide_rows(d, n_seq, q_len, q_heads))
         return civic::kQwStatusBytes + (size_t)2 * civic::kQwMaxBlocks * civic::qw_slot_floats(d.head_dim) * 4;
     if (whole_items(d, max_pages)) return 0;
     const int nt = attention_tiles(d, (int64_t)q_len * (q_heads / d.n_heads));
@@ -384,7 +387,7 @@ size_t civic_quant_attention_workspace_bytes(const civic_quant_desc_t* desc, int
                                              int32_t q_len, int32_t q_heads)
 {
     if (check_attention(desc, n_seq, q_len, q_heads) != CIVIC_OK || max_pages_per_seq < 0) return 0;
-    return attention_workspace(*desc, max_pages_per_seq, q_len, q_heads);
+    return attention_workspace(*desc, max_pages_per_seq, n_seq, q_len, q_heads);
 }
 
 civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q_strides, const void* cache,
@@ -405,7 +408,7 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     if (!aligned(q, 16) || !aligned(cache, 16) || !aligned(out, 16) || !aligned(block_table, 4) || !aligned(lens, 4) ||
         !aligned(q_lens, 4) || !aligned(lse, 4))
         return CIVIC_ERR_ALIGNMENT;
-    const size_t need = attention_workspace(d, max_pages_per_seq, q_len, q_heads);
+    const size_t need = attention_workspace(d, max_pages_per_seq, n_seq, q_len, q_heads);
     if (need > 0) {
         if (!workspace || workspace_bytes < need) return CIVIC_ERR_WORKSPACE;
         if (!aligned(workspace, 256)) return CIVIC_ERR_ALIGNMENT;
@@ -457,7 +460,7 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     const unsigned items = (unsigned)((rows + 8 * nt - 1) / (8 * nt) * d.n_heads);
     // a block's share of the tiles, of at least 148 blocks', is counted in 32 bits
     if ((double)n_seq * items * (p.capacity / civic::kQuantTile) > 148.0 * (1 << 30)) return CIVIC_ERR_UNSUPPORTED;
-    if (wide_rows(d, q_len, q_heads)) return launch_attention_wide_dim(d, p, rows, (cudaStream_t)stream);
+    if (wide_rows(d, n_seq, q_len, q_heads)) return launch_attention_wide_dim(d, p, rows, (cudaStream_t)stream);
     return d.dtype == CIVIC_BF16 ? launch_attention_dim<__nv_bfloat16>(d, nt, p, items, (cudaStream_t)stream)
                                  : launch_attention_dim<__half>(d, nt, p, items, (cudaStream_t)stream);
 }

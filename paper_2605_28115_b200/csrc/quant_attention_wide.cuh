@@ -644,19 +644,20 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
         auto scores = [&](int t, int h, int st) {
             const uint32_t d = uni(tmem + 128u * t + 64u * h), a0 = uni((uint32_t)desc_q + (uint32_t)((t * kTileBytes) >> 4));
             const uint32_t b0 = uni((uint32_t)desc_k + (uint32_t)((st * kTileBytes + h * 8192) >> 4));
-#pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk) {
-                const uint32_t step = (uint32_t)(kk >> 2) * 1024u + 2u * (uint32_t)(kk & 3);
-#pragma unroll
-                for (int part = 0; part < kParts; ++part)
-                    if (elect_one())
-                        umma_bf16(d, desc(hi_q, a0 + step), desc(hi_k, b0 + step + (uint32_t)(part * (kTileBytes >> 4))), idesc_s,
-                                  (kk | part) != 0);
-            }
             const uint32_t am = uni((uint32_t)desc_qm + (uint32_t)((t * kQwMidBytes) >> 4));
             const uint32_t bm = uni((uint32_t)desc_km + (uint32_t)((st * kQwMidBytes + h * 2048) >> 4));
-            if (elect_one()) umma_bf16(d, desc(hi_m, am), desc(hi_m, bm), idesc_s, 1);
-            if (elect_one()) umma_commit(&sy.s_full[t][h]);
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < HD / 16; ++kk) {
+                    const uint32_t step = (uint32_t)(kk >> 2) * 1024u + 2u * (uint32_t)(kk & 3);
+#pragma unroll
+                    for (int part = 0; part < kParts; ++part)
+                        umma_bf16(d, desc(hi_q, a0 + step), desc(hi_k, b0 + step + (uint32_t)(part * (kTileBytes >> 4))), idesc_s,
+                                  (kk | part) != 0);
+                }
+                umma_bf16(d, desc(hi_m, am), desc(hi_m, bm), idesc_s, 1);
+                umma_commit(&sy.s_full[t][h]);
+            }
             __syncwarp();
         };
         bool ok = true;
@@ -682,10 +683,12 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                     const uint32_t d = uni(tmem + 256u + 128u * t), a = uni(tmem + 128u * t + 64u * h);
                     const uint32_t b0 = uni((uint32_t)desc_v + (uint32_t)((st * kTileBytes + h * 8192) >> 4));
                     const uint32_t keep = uni(b + h > 0);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < kQwBlock / 32; ++kk)
-                        if (elect_one()) umma_bf16_a_tmem(d, a + 8u * kk, desc(hi_v, b0 + 128u * kk), idesc_o, kk != 0 ? 1u : keep);
-                    if (elect_one()) umma_commit(&sy.pv_done[t]);
+                        for (int kk = 0; kk < kQwBlock / 32; ++kk)
+                            umma_bf16_a_tmem(d, a + 8u * kk, desc(hi_v, b0 + 128u * kk), idesc_o, kk != 0 ? 1u : keep);
+                        umma_commit(&sy.pv_done[t]);
+                    }
                     __syncwarp();
                     if (more) {
                         if (part == 0 && !(ok = wait(&sy.k_full[k_next], k_next_phase, kAggTimeoutFull))) break;

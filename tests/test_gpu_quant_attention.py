@@ -64,7 +64,17 @@ class Setup:
         return read, rows
 
 
-def check(setup, q, out, lse, scale, causal, q_lens=None, canary=None, sample=None):
+def takes_tcgen05(setup, q):
+    return setup.dtype == torch.bfloat16 and setup.dim <= 128 and q.shape[1] * (q.shape[2] // setup.cache.n_heads) > 40 and \
+        q.shape[:3].numel() > 2048
+
+
+def many_rows(lens, q_len, q_heads):
+    """`lens` with empty slots behind, so that the batch has enough query rows for the tcgen05 kernels."""
+    return lens + [0] * max(0, 2049 // (q_len * q_heads) + 1 - len(lens))
+
+
+def check(setup, q, out, lse, scale, causal, q_lens=None, canary=None, sample=None, wide=None):
     """Tolerance of an output element: the rounding to T (eps / 2 of it); P' rounded to fp16 (2^-11 of the
     weighted sum of s * code, which is the output without the minima), elements of P' below 2^-14 of the
     largest to 2^-25 (2^-24 of the largest s * code a token); and the scores' error d, which moves each
@@ -75,7 +85,7 @@ def check(setup, q, out, lse, scale, causal, q_lens=None, canary=None, sample=No
     against 2^-7 of the tile's largest (2^-18 of it), and weights the same way (below 2^-14 of the largest by
     2^-25).  Their scores are exact products but for K groups whose scale is below 2^-5 of the tile's largest S:
     such a scale is off by at most 2^-25 against 2^-9 (2^-16 S), a value of up to 16 of them by 2^-12 S."""
-    wide = setup.dtype == torch.bfloat16 and setup.dim <= 128 and q.shape[1] * (q.shape[2] // setup.cache.n_heads) > 16
+    wide = takes_tcgen05(setup, q) if wide is None else wide
     read, rows = setup.reader()
     eps = torch.finfo(setup.dtype).eps / 2
     for s, n in enumerate(setup.lens_host):
@@ -156,7 +166,7 @@ def test_against_64_bits(case, causal, spare):
 
 
 WIDE = [  # lens, heads, q_heads, dim, bits, page, q_len
-    ([1], 1, 32, 128, 4, 16, 1),
+    ([1], 1, 48, 128, 4, 16, 1),
     ([40], 1, 20, 64, 8, 16, 40),
     ([127, 128, 129, 0, 300], 2, 8, 128, 4, 16, 33),
     ([500, 20, 61], 2, 14, 64, 4, 48, 61),
@@ -172,8 +182,9 @@ WIDE = [  # lens, heads, q_heads, dim, bits, page, q_len
 @pytest.mark.parametrize("causal", [True, False])
 def test_many_rows_against_64_bits(case, causal):
     lens, heads, q_heads, dim, bits, page, q_len = case
-    setup = Setup(lens, heads, dim, bits, page, torch.bfloat16, seed=23)
+    setup = Setup(many_rows(lens, q_len, q_heads), heads, dim, bits, page, torch.bfloat16, seed=23)
     q = setup.queries(q_len, q_heads)
+    assert takes_tcgen05(setup, q)
     out, lse = attend(setup, q, causal=causal)
     check(setup, q, out, lse, dim**-0.5, causal, sample=200)
     again, lse2 = attend(setup, q, causal=causal)
@@ -190,6 +201,7 @@ def test_many_rows_against_64_bits(case, causal):
 def test_many_rows_padded_batch():
     setup = Setup([400, 130, 100, 0, 31], 2, 128, 4, 16, torch.bfloat16, seed=24)
     q = setup.queries(70, 8)
+    assert takes_tcgen05(setup, q)
     for q_lens in ([70, 1, 0, 2, 64], [33, 64, 70, 0, 70], [1, 65, 64, 70, -4]):
         some = torch.tensor(q_lens, dtype=torch.int32, device=DEV)
         out = torch.full((5, 70, 8, 128), 7.0, dtype=torch.bfloat16, device=DEV)
@@ -203,7 +215,8 @@ def test_many_rows_many_items():
     lens = [int(x) for x in rng.integers(0, 200, 70)]
     lens[33] = 3000
     setup = Setup(lens, 2, 64, 4, 16, torch.bfloat16, seed=25)
-    q = setup.queries(9, 6)
+    q = setup.queries(9, 12)
+    assert takes_tcgen05(setup, q)
     out, lse = attend(setup, q)
     check(setup, q, out, lse, 0.125, True, sample=12)
 
@@ -214,26 +227,30 @@ def test_many_rows_masked_tokens_may_hold_anything():
         k[0, 150:], v[0, 150:] = float("nan"), float("inf")
         v[0, 145] = float("nan")
 
-    setup = Setup([160], 2, 64, 4, 16, torch.bfloat16, seed=26, edit=edit)
+    setup = Setup(many_rows([160], 20, 8), 2, 64, 4, 16, torch.bfloat16, seed=26, edit=edit)
     q = setup.queries(20, 8)  # tokens 140 .. 159
+    assert takes_tcgen05(setup, q)
 
     def same_rows(k, v):
         k[0], v[0] = setup.k[0, :145].float(), setup.v[0, :145].float()
 
     out, lse = attend(setup, q)
     clean = Setup([145], 2, 64, 4, 16, torch.bfloat16, seed=26, edit=same_rows)
-    check(clean, q[:, :5], out[:, :5], lse[:, :5], 0.125, True)
-    assert bool(torch.isnan(out[:, 5:]).all()) and bool(torch.isnan(lse[:, 10:]).all())
+    check(clean, q[:1, :5], out[:1, :5], lse[:1, :5], 0.125, True, wide=True)
+    assert bool(torch.isnan(out[:1, 5:]).all()) and bool(torch.isnan(lse[:1, 10:]).all())
+    assert bool((out[1:] == 0).all()) and bool((lse[1:] == -math.inf).all())
 
 
 def test_many_rows_nan_in_v_stays_in_its_group_where_all_see_it():
     def edit(k, v):
         v[0, 20, 1, 40] = float("nan")
 
-    setup = Setup([400], 2, 128, 8, 16, torch.bfloat16, seed=27, edit=edit)
-    out, lse = attend(setup, setup.queries(10, 8))
-    assert bool(torch.isnan(out[0, :, 4:, 32:64]).all()) and bool(torch.isfinite(lse).all())
-    assert int(torch.isnan(out).sum()) == 10 * 4 * 32
+    setup = Setup(many_rows([400], 11, 8), 2, 128, 8, 16, torch.bfloat16, seed=27, edit=edit)
+    q = setup.queries(11, 8)
+    assert takes_tcgen05(setup, q)
+    out, lse = attend(setup, q)
+    assert bool(torch.isnan(out[0, :, 4:, 32:64]).all()) and bool(torch.isfinite(lse[0]).all())
+    assert int(torch.isnan(out).sum()) == 11 * 4 * 32
 
 
 @pytest.mark.parametrize("bits", [4, 8])
@@ -254,18 +271,21 @@ def test_many_rows_extreme_ranges(bits, kind):
             k *= size
             v *= size.flip(1)
 
-    setup = Setup([277, 20], 1, 64, bits, 16, torch.bfloat16, seed=28, edit=edit, k_scale=8.0 if kind == "large_scores" else 1.0)
-    q = setup.queries(12, 3, {"large_scores": 60.0, "tiny_q": 2.0**-110, "zero_q": 0.0}.get(kind, 1.0))
+    setup = Setup(many_rows([277, 20], 14, 3), 1, 64, bits, 16, torch.bfloat16, seed=28, edit=edit,
+                  k_scale=8.0 if kind == "large_scores" else 1.0)
+    q = setup.queries(14, 3, {"large_scores": 60.0, "tiny_q": 2.0**-110, "zero_q": 0.0}.get(kind, 1.0))
     if kind == "sink":
         q = q.abs() * 2
     scale = {"tiny_q": 2.0**105, "negative": -0.2}.get(kind, 0.125)
+    assert takes_tcgen05(setup, q)
     out, lse = attend(setup, q, scale=scale)
     check(setup, q, out, lse, scale, True)
 
 
 def test_many_rows_bad_pages_are_left_out():
-    setup = Setup([300], 2, 128, 4, 16, torch.bfloat16, seed=29)
-    q = setup.queries(8, 8)
+    setup = Setup(many_rows([300], 12, 8), 2, 128, 4, 16, torch.bfloat16, seed=29)
+    q = setup.queries(12, 8)
+    assert takes_tcgen05(setup, q)
     for bad in (-1, setup.cache.n_pages, 2**31 - 1):
         setup.table[0, 2] = bad
         record = torch.zeros(4, dtype=torch.int32, device=DEV)
@@ -281,10 +301,12 @@ def test_many_rows_bad_pages_are_left_out():
 
 
 def test_many_rows_captured_and_replayed_and_on_two_streams():
-    setup = Setup([600, 290], 2, 128, 4, 16, torch.bfloat16, seed=30)
+    setup = Setup(many_rows([600, 290], 30, 8), 2, 128, 4, 16, torch.bfloat16, seed=30)
+    n_seq = len(setup.lens_host)
     q = setup.queries(30, 8).to(DEV)
+    assert takes_tcgen05(setup, q)
     out = torch.empty_like(q)
-    need = civic.quant_attention_workspace_bytes(setup.cache, setup.table.shape[1], 2, 30, 8)
+    need = civic.quant_attention_workspace_bytes(setup.cache, setup.table.shape[1], n_seq, 30, 8)
     ws = [torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(3)]
     lens = setup.lens.clone()
     run = lambda: civic.civic_quant_attention(q, setup.cache, 0, setup.table, lens, out=out, workspace=ws[0])
@@ -294,7 +316,7 @@ def test_many_rows_captured_and_replayed_and_on_two_streams():
     with torch.cuda.graph(graph):
         run()
     for now in ([600, 290], [30, 64], [0, 289], [7, 0]):
-        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        lens.copy_(torch.tensor(now + [0] * (n_seq - 2), dtype=torch.int32))
         out.fill_(5)
         graph.replay()
         torch.cuda.synchronize()
