@@ -468,8 +468,8 @@ civic_status_t civic_kv_compressed_attention_prepared(const void* q, const void*
  *
  * head_dim 64, 128 or 256; bits 4 or 8; page_size a multiple of 16 up to 1024; up to 1024 heads;
  * dtype the 16-bit type of the rows, of q and out, and of the parameters: CIVIC_ERR_UNSUPPORTED
- * otherwise.  Pointers to rows and caches 16-byte aligned, strides multiples of 8 elements (rows that are
- * aligned to 32 bytes are read 32 bytes at a time).
+ * otherwise.  Pointers to rows and caches 16-byte aligned, strides multiples of 8 elements where the
+ * dimension is larger than 1 (rows that are aligned to 32 bytes are read 32 bytes at a time).
  *
  * Pages.  Token i of sequence s lives in page block_table[s, i / page_size].  Entries a call does not
  * need may hold anything.  A page outside [0, n_pages), or a token behind the table's last entry, is
@@ -568,10 +568,12 @@ civic_status_t civic_read_kv_quant(const void* const* cache, const civic_quant_d
  * workspace   dev scratch of civic_quant_attention_workspace_bytes(...) bytes, 256-byte aligned (NULL where
  *             that is 0); contents on entry are irrelevant.  Calls that may overlap on the GPU need
  *             separate workspaces
- * Weights and codes are multiplied as fp16 with fp32 accumulation, scores, sums and lse are fp32.  V
- * groups' scales are expected within 2^-86 .. 2^100, scores may have any size; max_pages_per_seq *
- * page_size <= 2^30 (CIVIC_ERR_UNSUPPORTED).  One launch where
- * max_pages_per_seq * page_size <= 1024, two otherwise.
+ * Codes and weights are multiplied as fp16 with fp32 accumulation; scores, sums and lse are fp32.  Scores
+ * may have any size; magnitudes in the cache are expected below 2^100 and V groups' scales above 2^-86.
+ * max_pages_per_seq * page_size <= 2^30, q_len * q_heads <= 2^24, n_seq <= 65535 (CIVIC_ERR_UNSUPPORTED).
+ * One launch (max_pages_per_seq * page_size <= 1024) or two.  With many query rows (bf16, head_dim up to
+ * 128) tcgen05 kernels run: a NaN in V may then make a whole row of the last q_len tokens NaN, not its
+ * group alone, and should a wait inside them run into its limit of about a second, out and lse are NaN.
  */
 civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q_strides, const void* cache,
                                      const civic_quant_desc_t* desc, const int32_t* block_table, int32_t max_pages_per_seq,

@@ -35,13 +35,18 @@ size_t extent_bytes(const civic_row_strides_t& s, int64_t n_seq, int64_t rows, i
     return (size_t)((n_seq - 1) * s.seq + (rows - 1) * s.token + (heads - 1) * s.head + head_dim) * 2;
 }
 
-// Strides: multiples of 16 bytes, not negative; no overflow of the address arithmetic.
-civic_status_t check_strides(const civic_row_strides_t* s)
+// Strides: multiples of 16 bytes, not negative; no overflow of the address arithmetic.  The stride of a
+// dimension of size 1 is not used and may be anything: `used` gets 0 for it.
+civic_status_t check_strides(const civic_row_strides_t* given, int64_t n_seq, int64_t rows, int64_t heads, civic_row_strides_t& used)
 {
-    if (!s || s->seq < 0 || s->token < 0 || s->head < 0) return CIVIC_ERR_INVALID_ARG;
-    if (s->seq % 8 || s->token % 8 || s->head % 8) return CIVIC_ERR_ALIGNMENT;
+    if (!given) return CIVIC_ERR_INVALID_ARG;
+    used.seq = n_seq > 1 ? given->seq : 0;
+    used.token = rows > 1 ? given->token : 0;
+    used.head = heads > 1 ? given->head : 0;
+    if (used.seq < 0 || used.token < 0 || used.head < 0) return CIVIC_ERR_INVALID_ARG;
+    if (used.seq % 8 || used.token % 8 || used.head % 8) return CIVIC_ERR_ALIGNMENT;
     const int64_t limit = (int64_t)1 << 40;
-    if (s->seq > limit || s->token > limit || s->head > limit) return CIVIC_ERR_UNSUPPORTED;
+    if (used.seq > limit || used.token > limit || used.head > limit) return CIVIC_ERR_UNSUPPORTED;
     return CIVIC_OK;
 }
 
@@ -128,9 +133,10 @@ civic_status_t move_impl(const MoveCall& c, void* stream_)
     civic_status_t st = check_desc(c.desc);
     if (st != CIVIC_OK) return st;
     if (c.n_layers < 1 || c.n_seq < 0 || c.n_rows < 0 || c.max_pages < 0) return CIVIC_ERR_INVALID_ARG;
-    st = check_strides(c.strides);
-    if (st != CIVIC_OK) return st;
     const civic_quant_desc_t& d = *c.desc;
+    civic_row_strides_t strides;
+    st = check_strides(c.strides, c.n_seq, c.wide_rows, d.n_heads, strides);
+    if (st != CIVIC_OK) return st;
     if (c.n_seq == 0 || c.n_rows == 0) return CIVIC_OK;
     if (!c.k || !c.v || !c.cache || !c.block_table) return CIVIC_ERR_INVALID_ARG;
     if (!aligned(c.block_table, 4) || !aligned(c.idx, 4) || !aligned(c.start, 4) || !aligned(c.counts, 4))
@@ -140,9 +146,9 @@ civic_status_t move_impl(const MoveCall& c, void* stream_)
         if (!aligned(c.k[l], 16) || !aligned(c.v[l], 16) || !aligned(c.cache[l], 16)) return CIVIC_ERR_ALIGNMENT;
         if (!c.writes_cache && c.k[l] == c.v[l]) return CIVIC_ERR_INVALID_ARG;
     }
-    if (!c.writes_cache && !writable_strides(*c.strides, c.n_seq, c.n_rows, d.n_heads, d.head_dim)) return CIVIC_ERR_INVALID_ARG;
+    if (!c.writes_cache && !writable_strides(strides, c.n_seq, c.n_rows, d.n_heads, d.head_dim)) return CIVIC_ERR_INVALID_ARG;
     if (c.wide_rows > 0) {
-        const size_t wide = extent_bytes(*c.strides, c.n_seq, c.wide_rows, d.n_heads, d.head_dim);
+        const size_t wide = extent_bytes(strides, c.n_seq, c.wide_rows, d.n_heads, d.head_dim);
         const size_t cache = (size_t)d.n_pages * page_bytes(d);
         if (lists_overlap(c.k, c.n_layers, wide, c.cache, c.n_layers, cache) ||
             lists_overlap(c.v, c.n_layers, wide, c.cache, c.n_layers, cache))
@@ -180,9 +186,9 @@ civic_status_t move_impl(const MoveCall& c, void* stream_)
     p.start = c.start;
     p.counts = c.counts;
     p.block_table = c.block_table;
-    p.seq_stride = c.strides->seq * 2;
-    p.token_stride = c.strides->token * 2;
-    p.head_stride = c.strides->head * 2;
+    p.seq_stride = strides.seq * 2;
+    p.token_stride = strides.token * 2;
+    p.head_stride = strides.head * 2;
     p.n_units = (uint32_t)units;
     p.n_heads = d.n_heads;
     p.tiles = (int32_t)tiles;
@@ -228,7 +234,9 @@ civic_status_t launch_attention(civic::QuantAttnParams& p, unsigned items, cudaS
 {
     const bool pdl = programmatic();
     static std::atomic<int> allowed[2][64], resident[64];
-    if (p.blocks == 0) {
+    // Eight warps to an item while every SM gets at most one (128 items of 26 tiles: 7.0 us, with four warps 8.8);
+    // beyond that more and smaller blocks, of which four share an SM (512 items of 63 tiles: 28 us instead of 40).
+    if (p.blocks == 0 && (int64_t)items * p.n_seq <= sm_count()) {
         constexpr int kWarps = civic::kQaWholeWarps;
         const auto kernel = civic::quant_attention_kernel<T, HD, BITS, NT, kWarps>;
         constexpr size_t smem = civic::qa_smem_bytes<HD, BITS, NT, kWarps>();
@@ -244,6 +252,11 @@ civic_status_t launch_attention(civic::QuantAttnParams& p, unsigned items, cudaS
     constexpr size_t smem = civic::qa_smem_bytes<HD, BITS, NT, kWarps>();
     const civic_status_t as = allow_dynamic_smem(kernel, smem, allowed[1]);
     if (as != CIVIC_OK) return as;
+    if (p.blocks == 0) {
+        CIVIC_CUDA_TRY(civic::launch(pdl, kernel, dim3(items, (unsigned)p.n_seq), 32u * kWarps, smem, stream, p));
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+        return CIVIC_OK;
+    }
     const int dev = device_slot();
     int per_sm = dev >= 0 ? resident[dev].load(std::memory_order_relaxed) : 0;
     if (per_sm == 0) {
@@ -398,7 +411,8 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
 {
     civic_status_t st = check_attention(desc, n_seq, q_len, q_heads);
     if (st != CIVIC_OK) return st;
-    st = check_strides(q_strides);
+    civic_row_strides_t strides;
+    st = check_strides(q_strides, n_seq, q_len, q_heads, strides);
     if (st != CIVIC_OK) return st;
     if (max_pages_per_seq < 0 || !std::isfinite(scale)) return CIVIC_ERR_INVALID_ARG;
     const civic_quant_desc_t& d = *desc;
@@ -418,7 +432,7 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
         const void* made[3] = {out, lse, workspace};
         const size_t made_bytes[3] = {rows * d.head_dim * 2, rows * 4, need};
         const void* given[5] = {q, cache, block_table, lens, q_lens};
-        const size_t given_bytes[5] = {extent_bytes(*q_strides, n_seq, q_len, q_heads, d.head_dim), (size_t)d.n_pages * page_bytes(d),
+        const size_t given_bytes[5] = {extent_bytes(strides, n_seq, q_len, q_heads, d.head_dim), (size_t)d.n_pages * page_bytes(d),
                                        (size_t)n_seq * max_pages_per_seq * 4, (size_t)n_seq * 4, (size_t)n_seq * 4};
         for (int a = 0; a < 3; ++a) {
             for (int b = 0; b < 5; ++b)
@@ -437,9 +451,9 @@ civic_status_t civic_quant_attention(const void* q, const civic_row_strides_t* q
     p.out = (char*)out;
     p.lse = lse;
     p.partial = (float*)workspace;
-    p.q_seq = q_strides->seq * 2;
-    p.q_token = q_strides->token * 2;
-    p.q_head = q_strides->head * 2;
+    p.q_seq = strides.seq * 2;
+    p.q_token = strides.token * 2;
+    p.q_head = strides.head * 2;
     p.n_seq = n_seq;
     p.q_len = q_len;
     p.q_heads = q_heads;

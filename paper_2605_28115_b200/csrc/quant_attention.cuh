@@ -36,8 +36,8 @@
 
 namespace civic {
 
-constexpr int kQaWarps = 4;        // warps of a block where items are shared
-constexpr int kQaWholeWarps = 8;   // and where a block takes an item as a whole: 128 items of 26 tiles 8.8 -> 7.0 us
+constexpr int kQaWarps = 4;        // warps of a block
+constexpr int kQaWholeWarps = 8;   // where a block takes an item as a whole and items are few
 constexpr int kQaMaxBlocks = 148 * 4;  // also fixes the workspace size
 constexpr int kQaMinTiles = 2 * kQaWarps;
 constexpr int kQaWholeTiles = 64;      // tables up to this many tiles: a block per item, nothing to join
@@ -250,7 +250,9 @@ struct QaWarp {
     using H = Half16<T>;
     static constexpr int NG = Tile::kGroups, MT = HD / 16;
 
-    uint32_t q[NT][NG][2][2];  // operand of the first product: [group][depth step][register]
+    // Operand of the first product, the same for the block's warps: in shared memory, [n-tile][group][depth step][lane]
+    // (16 registers fewer per tile of 8 rows make room for a fourth block per SM)
+    const uint2* q;
     uint32_t q_sum[NT][(NG + 3) / 4][2];  // operand that meets the minima: the sum over group t (+ 4) of q in three parts
     float factor[NT][2];       // takes a raw score to base-2 logits
     int limit[NT][2];          // tokens the column's query row sees
@@ -279,8 +281,11 @@ struct QaWarp {
         }
     }
 
-    __device__ __forceinline__ void begin(const QuantAttnParams& p, const QaCursor& c, const uint4 (&xs)[NT][NG])
+    // `first`: this warp writes the shared operand; the block has to synchronise before the first step.
+    __device__ __forceinline__ void begin(const QuantAttnParams& p, const QaCursor& c, const uint4 (&xs)[NT][NG], uint2* q_shared,
+                                          bool first)
     {
+        q = q_shared + (threadIdx.x & 31);
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         const int head = c.item / c.q.row_blocks, row0 = (c.item - head * c.q.row_blocks) * (8 * NT);
         const int rows = c.q.q_len * p.group;
@@ -317,17 +322,15 @@ struct QaWarp {
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
                 sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
                 sums[j] = sum * kSumUnit;
-                if constexpr (BITS == 4) {
-                    // nibbles i and i + 4 of a word meet in one operand register; odd ones arrive times 16
-                    q[nt][j][0][0] = pack_half2(f[j][0], f[j][4]);
-                    q[nt][j][0][1] = pack_half2(f[j][1] * 0.0625f, f[j][5] * 0.0625f);
-                    q[nt][j][1][0] = pack_half2(f[j][2], f[j][6]);
-                    q[nt][j][1][1] = pack_half2(f[j][3] * 0.0625f, f[j][7] * 0.0625f);
-                } else {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        q[nt][j][h][0] = pack_half2(f[j][4 * h], f[j][4 * h + 2]);
-                        q[nt][j][h][1] = pack_half2(f[j][4 * h + 1], f[j][4 * h + 3]);
+                if (first) {
+                    uint2* to = q_shared + (nt * NG + j) * 64 + lane;
+                    if constexpr (BITS == 4) {
+                        // nibbles i and i + 4 of a word meet in one operand register; odd ones arrive times 16
+                        to[0] = make_uint2(pack_half2(f[j][0], f[j][4]), pack_half2(f[j][1] * 0.0625f, f[j][5] * 0.0625f));
+                        to[32] = make_uint2(pack_half2(f[j][2], f[j][6]), pack_half2(f[j][3] * 0.0625f, f[j][7] * 0.0625f));
+                    } else {
+                        to[0] = make_uint2(pack_half2(f[j][0], f[j][2]), pack_half2(f[j][1], f[j][3]));
+                        to[32] = make_uint2(pack_half2(f[j][4], f[j][6]), pack_half2(f[j][5], f[j][7]));
                     }
                 }
             }
@@ -443,8 +446,10 @@ struct QaWarp {
                     for (int nt = 0; nt < NT; ++nt) {
                         float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            mma_16x8x16(d, a[h][0], a[h][1], a[h][2], a[h][3], q[nt][j][h][0], q[nt][j][h][1]);
+                        for (int h = 0; h < 2; ++h) {
+                            const uint2 b = q[(nt * NG + j) * 64 + h * 32];
+                            mma_16x8x16(d, a[h][0], a[h][1], a[h][2], a[h][3], b.x, b.y);
+                        }
 #pragma unroll
                         for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -627,14 +632,14 @@ struct QaWarp {
 template <int HD, int BITS>
 __host__ __device__ constexpr int qa_stages()
 {
-    const int n = 12288 / quant_tile_bytes(HD, BITS);
+    const int n = 8192 / quant_tile_bytes(HD, BITS);
     return n < 2 ? 2 : (n > 6 ? 6 : n);
 }
-// ring | O of every warp, one n-tile at a time | reference and sum of every warp and row
+// ring | O of every warp, one n-tile at a time | reference and sum of every warp and row | the queries' operand
 template <int HD, int BITS, int NT, int W>
 __host__ __device__ constexpr size_t qa_smem_bytes()
 {
-    return (size_t)W * (qa_stages<HD, BITS>() * quant_tile_bytes(HD, BITS) + 8 * HD * 4 + NT * 8 * 8);
+    return (size_t)W * (qa_stages<HD, BITS>() * quant_tile_bytes(HD, BITS) + 8 * HD * 4 + NT * 8 * 8) + NT * (HD / 32) * 512;
 }
 
 // out and lse of one row from the sums over its tokens
@@ -654,7 +659,7 @@ __device__ __forceinline__ void qa_store(const QuantAttnParams& p, int seq, int 
 template <int HD, int NT>
 __host__ __device__ constexpr int qa_min_blocks()
 {
-    return HD * NT <= 64 ? 4 : (HD * NT <= 128 ? 3 : 2);
+    return HD * NT <= 128 ? 4 : 2;
 }
 
 template <typename T, int HD, int BITS, int NT, int W>
@@ -666,6 +671,7 @@ __global__ void __launch_bounds__(32 * W, W == kQaWarps ? qa_min_blocks<HD, NT>(
     uint8_t* ring_all = qa_smem;
     float* o_sm = reinterpret_cast<float*>(qa_smem + W * kStages * Tile::kBytes);  // [warp][8][HD]
     float2* ml_sm = reinterpret_cast<float2*>(o_sm + W * 8 * HD);                  // [warp][rows]
+    uint2* q_sm = reinterpret_cast<uint2*>(ml_sm + W * kRows);
     const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     uint8_t* ring = ring_all + warp * kStages * Tile::kBytes;
     release_next_kernel();  // the joining kernel is small: its blocks may wait beside this one's
@@ -749,7 +755,8 @@ __global__ void __launch_bounds__(32 * W, W == kQaWarps ? qa_min_blocks<HD, NT>(
     do {
         // one item's tiles inside this block's share
         const int taken = min(units - at, cur.q.tiles - cur.tile);
-        w.begin(p, cur, x);
+        w.begin(p, cur, x, q_sm, warp == 0);
+        __syncthreads();
         int sees_all = w.limit[0][0];  // tokens that every column of the warp sees
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sees_all = min(sees_all, min(w.limit[nt][0], w.limit[nt][1]));

@@ -395,6 +395,63 @@ def test_extreme_ranges(bits, kind):
     check(setup, q, out, lse, 2.0**105 if kind == "tiny_q" else 0.125, True)
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("kind", ["large_scores", "sink", "tiny_v", "equal_rows", "flat"])
+def test_extreme_ranges_in_fp16(bits, dim, kind):
+    def edit(k, v):
+        if kind == "sink":
+            k[:, 3] = -4.0
+            v[:, 3] *= 2.0**10
+        elif kind == "tiny_v":  # scales among fp16's subnormals
+            v *= 2.0**-12
+        elif kind == "equal_rows":
+            k[:], v[:] = 1.25, -3.5
+        elif kind == "flat":  # scores alike: sums of many weights
+            k *= 0.01
+
+    setup = Setup([1900, 20] if kind == "flat" else [177, 20], 1, dim, bits, 16, torch.float16, seed=31, edit=edit,
+                  k_scale=8.0 if kind == "large_scores" else 1.0)
+    q = setup.queries(5, 5, 60.0 if kind == "large_scores" else 1.0)
+    if kind == "sink":
+        q = q.abs() * 2
+    out, lse = attend(setup, q)
+    check(setup, q, out, lse, dim**-0.5, True)
+
+
+def test_strides_of_dimensions_of_size_one_do_not_matter():
+    setup = Setup([50], 1, 128, 4, 16, torch.bfloat16, seed=32)
+    q = setup.queries(1, 1).to(DEV)
+    want, _ = civic.civic_quant_attention(q, setup.cache, 0, setup.table, setup.lens)
+    odd = q.as_strided((1, 1, 1, 128), (3, 5, 7, 1))
+    got, _ = civic.civic_quant_attention(odd, setup.cache, 0, setup.table, setup.lens)
+    assert torch.equal(got, want)
+    before = setup.cache.buffer.clone()
+    x = setup.k[None, :, 40:41].to(DEV)
+    start = torch.tensor([40], dtype=torch.int32, device=DEV)
+    y = setup.v[None, :, 40:41].to(DEV)
+    civic.civic_append_kv_quant(x.as_strided((1, 1, 1, 1, 128), (9, 3, 5, 7, 1)), y.as_strided((1, 1, 1, 1, 128), (9, 3, 5, 7, 1)),
+                                start, setup.cache, setup.table)
+    assert torch.equal(setup.cache.buffer, before)
+
+
+def test_empty_batches():
+    setup = Setup([20], 2, 128, 4, 16, torch.bfloat16, seed=33)
+    before = civic.launch_count()
+    none = torch.empty((0,), dtype=torch.int32, device=DEV)
+    table = torch.empty((0, 4), dtype=torch.int32, device=DEV)
+    out, lse = civic.civic_quant_attention(torch.empty((0, 3, 4, 128), dtype=torch.bfloat16, device=DEV), setup.cache, 0, table, none,
+                                           want_lse=True)
+    assert out.shape == (0, 3, 4, 128) and lse.shape == (0, 3, 4)
+    out, _ = civic.civic_quant_attention(torch.empty((1, 0, 4, 128), dtype=torch.bfloat16, device=DEV), setup.cache, 0, setup.table,
+                                         setup.lens)
+    assert out.shape == (1, 0, 4, 128) and civic.launch_count() == before
+    # a block table without entries: every sequence is empty
+    out, lse = civic.civic_quant_attention(setup.queries(2, 4).to(DEV), setup.cache, 0,
+                                           torch.empty((1, 0), dtype=torch.int32, device=DEV), setup.lens, want_lse=True)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
 def test_q_slices_scale_and_given_buffers():
     setup = Setup([1030, 64], 2, 128, 4, 32, torch.bfloat16, seed=8)
     fused = torch.randn((2, 3, 4 + 2 + 2, 128), generator=setup.gen).to(torch.bfloat16)

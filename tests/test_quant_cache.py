@@ -101,7 +101,7 @@ def compact(lib, k=(K,), v=(V,), st=None, n_layers=1, n_seq=1, seq_len=40, s_out
                                       d or desc(), tab, pages, None)
 
 
-def append(lib, k=(K,), v=(V,), st=None, n_layers=1, n_seq=1, n_new=1, start=IDX, counts=None, cache=(C,), d=None, tab=TAB,
+def append(lib, k=(K,), v=(V,), st=None, n_layers=1, n_seq=1, n_new=2, start=IDX, counts=None, cache=(C,), d=None, tab=TAB,
            pages=2):
     return lib.civic_append_kv_quant(ptrs(*k), ptrs(*v), st or strides(), n_layers, n_seq, n_new, start, counts, ptrs(*cache),
                                      d or desc(), tab, pages, None)
@@ -155,7 +155,7 @@ def test_row_calls_refuse_on_the_host(lib):
         assert call(lib, cache=(C + 4,)) == ALIGN
         assert call(lib, st=strides(token=-256)) == ARG
         assert call(lib, st=strides(token=260)) == ALIGN
-        assert call(lib, st=strides(seq=1 << 50)) == UNSUP
+        assert call(lib, st=strides(token=1 << 50)) == UNSUP
         assert call(lib, k=(C + 16,)) == ARG  # rows inside the cache
         assert call(lib, n_seq=1 << 30, st=strides(seq=0)) in (UNSUP, ARG)
         assert call(lib, n_seq=0, k=(None,), tab=None) == OK
