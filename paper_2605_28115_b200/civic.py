@@ -14,6 +14,7 @@ import functools
 import os
 from typing import Optional, Sequence
 
+import numpy as np
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -801,8 +802,7 @@ class QuantCache:
     def tables(self) -> ctypes.Array:
         """Host pointer table of the layers."""
         if self._tables is None:
-            self._tables = _pointer_array(self.n_layers)(*range(self.ptr, self.ptr + self.n_layers * self.layer_bytes,
-                                                                self.layer_bytes))
+            self._tables = _pointer_table(self.ptr, self.n_layers, self.layer_bytes)
         return self._tables
 
 
@@ -813,6 +813,13 @@ class QuantCache:
 def _pointer_array(n: int):
     """The type of n pointers."""
     return ctypes.c_void_p * n
+
+
+def _pointer_table(base: int, n: int, step: int) -> ctypes.Array:
+    """base, base + step, ... (n of them); through numpy, which counts faster than ctypes converts."""
+    if n == 1:
+        return _pointer_array(1)(base)
+    return _pointer_array(n).from_buffer(np.arange(n, dtype=np.uint64) * np.uint64(step) + np.uint64(base))
 
 
 @functools.lru_cache(maxsize=256)
@@ -860,7 +867,7 @@ def _rows_of(cache: QuantCache, x, what: str):
         if len(shape) != 5 or shape[0] != n:
             raise ValueError(f"{what} must be [n_layers, n_seq, rows, n_heads, head_dim]")
         first, base, shape = x, x.data_ptr(), shape[1:]
-        table = _pointer_array(n)(*range(base, base + 2 * n * step, 2 * step)) if n > 1 and step > 0 else _pointer_array(n)(*[base] * n)
+        table = _pointer_table(base, n, 2 * step)
     else:
         if len(x) != n or any(t.dim() != 4 for t in x):
             raise ValueError(f"{what} must be one [n_seq, rows, n_heads, head_dim] tensor per layer of the cache")
