@@ -10,8 +10,10 @@
 //   MMA        S_t = Q_t K'^T into tensor memory, t = 0, 1; then O_t += P_t V', P_t read from tensor memory
 //   softmax    maximum, exp2, P_t packed over S_t; O_t is rescaled only when a row's reference moved
 // Scores, weights and products go by halves of a block (64 tokens): while the softmax works on one half the
-// tensor cores multiply the other half's weights and fetch it the next scores, so that neither waits for
-// the other's latency (whole blocks: 237 us for the chunk below, halves: 185 us).
+// tensor cores multiply the other half's weights and make the next scores, so that neither waits for the
+// other's latency.  500 query tokens, 32 heads of 128, on 4 sequences of 4001 in 4 bits (123 GFLOP): 216 us =
+// 570 TFLOP/s, a third of the tensor cores' measured rate; softmax, MMA issue and producers are each busy for 70
+// to 85 % of the 6700 cycles that a unit of 256 rows x 128 tokens takes.
 //
 // fp16 operands, and scores without a rounding in them.  In the middle of its codes a group is
 //     k = s (c - 8) + (m + 8 s):
