@@ -779,8 +779,8 @@ class QuantCache:
     caller-owned; the format is civic.h's).  `dtype` (bfloat16 or float16) is the type of the rows, of the
     queries and of the outputs."""
 
-    __slots__ = ("buffer", "page_size", "head_dim", "bits", "dtype", "n_layers", "n_pages", "n_heads", "device", "desc_ref",
-                 "ptr", "layer_bytes", "_tables")  # desc_ref: the description as a C argument
+    __slots__ = ("buffer", "page_size", "head_dim", "bits", "dtype", "n_layers", "n_pages", "n_heads", "device", "index",
+                 "desc_ref", "ptr", "layer_bytes", "_tables")  # index: of the device; desc_ref: the description as a C argument
 
     def __init__(self, buffer: torch.Tensor, page_size: int, head_dim: int, bits: int, dtype: torch.dtype = torch.bfloat16):
         code = QUANT_DTYPES.get(dtype)
@@ -797,7 +797,7 @@ class QuantCache:
             raise ValueError("buffer's last dimension must be page_size / 16 * quant_tile_bytes(head_dim, bits)")
         self.layer_bytes = self.n_pages * page_bytes
         self.buffer, self.page_size, self.head_dim, self.bits, self.dtype = buffer, page_size, head_dim, bits, dtype
-        self.device, self._tables = buffer.device, None
+        self.device, self.index, self._tables = buffer.device, buffer.get_device(), None
 
     def tables(self) -> ctypes.Array:
         """Host pointer table of the layers."""
@@ -837,10 +837,9 @@ def _row_strides(seq: int, token: int, head: int):
 
 def _call(cache: "QuantCache", where: str, *args, stream: Optional[torch.cuda.Stream]) -> None:
     """One C call on the cache's device and on `stream` (default: torch's current one), the last argument."""
-    fn = getattr(load(), where)
-    index = cache.device.index
+    fn, index = getattr(_lib or load(), where), cache.index
     if _current_device() == index:
-        status = fn(*args, _stream_ptr(stream))
+        status = fn(*args, _raw_stream(index) if stream is None and _raw_stream is not None else _stream_ptr(stream))
     else:
         with torch.cuda.device(index):
             status = fn(*args, _stream_ptr(stream))
@@ -875,6 +874,9 @@ def _rows_of(cache: QuantCache, x, what: str):
         shape, strides = first.shape, first.stride()
         if any(t.shape != shape or t.stride() != strides or t.dtype != first.dtype or t.device != first.device for t in x):
             raise ValueError(f"all {what} tensors must share shape, strides, dtype and device")
+        if first.device != cache.device:  # each of them: one tensor may be pinned and the next not
+            for t in x:
+                _need_device(cache, t, what)
         table = _pointer_array(n)(*[t.data_ptr() for t in x])
     n_seq, rows, heads, dim = shape
     seq, token, head, last = strides
@@ -884,6 +886,17 @@ def _rows_of(cache: QuantCache, x, what: str):
     if first.device != cache.device:
         _need_device(cache, first, what)
     return table, (n_seq, rows), (seq, token, head)
+
+
+def _same_rows(cache: QuantCache, first, x, what: str):
+    """Pointer table of row tensors that must be laid out as `first` is, which _rows_of has looked at."""
+    if (isinstance(x, torch.Tensor) and isinstance(first, torch.Tensor) and x.shape == first.shape
+            and x.stride() == first.stride() and x.dtype is first.dtype and x.device == cache.device):
+        return _pointer_table(x.data_ptr(), cache.n_layers, 2 * x.stride(0))
+    table, *layout = _rows_of(cache, x, what)
+    if layout != list(_rows_of(cache, first, what)[1:]):
+        raise ValueError(f"{what} must share shape and strides with the other rows")
+    return table
 
 
 def _need_device(cache: QuantCache, x: torch.Tensor, what: str) -> None:
@@ -909,9 +922,7 @@ def civic_compact_kv_quant(k_src, v_src, seq_idx: torch.Tensor, cache: QuantCach
     k_src, v_src [n_layers, n_seq, seq_len, n_heads, head_dim] (or a sequence of per-layer tensors) with equal
     strides; seq_idx int32 [n_seq, s_out]; block_table int32 [n_seq, max_pages_per_seq]."""
     k, shape, strides = _rows_of(cache, k_src, "k_src")
-    v, *same = _rows_of(cache, v_src, "v_src")
-    if same != [shape, strides]:
-        raise ValueError("k_src and v_src must share shape and strides")
+    v = _same_rows(cache, k_src, v_src, "v_src")
     n_seq, seq_len = shape
     idx = _seq_words(cache, seq_idx, n_seq, "seq_idx", 2)
     table = _seq_words(cache, block_table, n_seq, "block_table", 2)
@@ -925,9 +936,7 @@ def civic_append_kv_quant(k_new, v_new, start: torch.Tensor, cache: QuantCache, 
     k_new, v_new [n_layers, n_seq, n_new, n_heads, head_dim] (or a sequence of per-layer tensors); start, counts
     int32 [n_seq]; block_table int32 [n_seq, max_pages_per_seq]."""
     k, shape, strides = _rows_of(cache, k_new, "k_new")
-    v, *same = _rows_of(cache, v_new, "v_new")
-    if same != [shape, strides]:
-        raise ValueError("k_new and v_new must share shape and strides")
+    v = _same_rows(cache, k_new, v_new, "v_new")
     n_seq, n_new = shape
     at = _seq_words(cache, start, n_seq, "start")
     some = _seq_words(cache, counts, n_seq, "counts")
@@ -942,9 +951,7 @@ def civic_read_kv_quant(cache: QuantCache, block_table: torch.Tensor, counts: to
     v_out [n_layers, n_seq, max_rows, n_heads, head_dim] (or sequences of per-layer tensors); the rows behind are
     left as they were.  counts, start int32 [n_seq].  Returns (k_out, v_out)."""
     k, shape, strides = _rows_of(cache, k_out, "k_out")
-    v, *same = _rows_of(cache, v_out, "v_out")
-    if same != [shape, strides]:
-        raise ValueError("k_out and v_out must share shape and strides")
+    v = _same_rows(cache, k_out, v_out, "v_out")
     n_seq, rows = shape
     some = _seq_words(cache, counts, n_seq, "counts")
     at = _seq_words(cache, start, n_seq, "start")
@@ -985,31 +992,44 @@ def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_
     max_pages = block_table.shape[1]
     made = []  # allocated here: not to be handed out again before `stream` is done with it
     if out is None:
-        out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=dev)
+        # empty_like is the quicker of the two; pinned queries have it make pageable memory
+        out = torch.empty_like(q) if q.device == dev and q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=dev)
         made.append(out)
-    elif out.shape != q.shape:
-        raise ValueError("out must have q's shape")
-    if lse is None:
-        if want_lse:
-            lse = out.new_empty((n_seq, q_len, q_heads), dtype=torch.float32)
-            made.append(lse)
-    elif lse.shape != q.shape[:3]:
-        raise ValueError("lse must be [n_seq, q_len, q_heads]")
-    lib = load()
+        out_ptr = out.data_ptr()
+    else:
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+        if out.device != dev:
+            _need_device(cache, out, "out")
+        out_ptr = _dev_ptr(out, "out", cache.dtype)
+    lse_ptr = None
+    if lse is not None:
+        if lse.shape != q.shape[:3]:
+            raise ValueError("lse must be [n_seq, q_len, q_heads]")
+        if lse.device != dev:
+            _need_device(cache, lse, "lse")
+        lse_ptr = _dev_ptr(lse, "lse", torch.float32)
+    elif want_lse:
+        lse = torch.empty((n_seq, q_len, q_heads), dtype=torch.float32, device=dev)
+        made.append(lse)
+        lse_ptr = lse.data_ptr()
+    ws_ptr, ws_bytes = None, 0
     if workspace is None:
-        need = lib.civic_quant_attention_workspace_bytes(cache.desc_ref, max_pages, n_seq, q_len, q_heads)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        ws_bytes = load().civic_quant_attention_workspace_bytes(cache.desc_ref, max_pages, n_seq, q_len, q_heads)
+        if ws_bytes:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
             made.append(workspace)
-    elif workspace.device != dev:
-        _need_device(cache, workspace, "workspace")
+            ws_ptr = workspace.data_ptr()
+    else:
+        if workspace.device != dev:
+            _need_device(cache, workspace, "workspace")
+        ws_ptr, ws_bytes = _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel()
     if stream is not None:
         for t in made:
             t.record_stream(stream)
     _call(cache, "civic_quant_attention", q.data_ptr(), _row_strides(seq, token, head), cache.ptr + layer * cache.layer_bytes,
           cache.desc_ref, table, max_pages, n_tok, n_q, n_seq, q_len, q_heads, dim ** -0.5 if scale is None else scale, causal,
-          _dev_ptr(out, "out", cache.dtype), _dev_ptr(lse, "lse", torch.float32), _dev_ptr(workspace, "workspace", torch.uint8),
-          0 if workspace is None else workspace.numel(), stream=stream)
+          out_ptr, lse_ptr, ws_ptr, ws_bytes, stream=stream)
     return out, lse
 
 

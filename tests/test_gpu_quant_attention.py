@@ -623,3 +623,52 @@ def test_wrong_shapes_devices_and_types_raise():
             civic.civic_append_kv_quant(k, v, start, setup.cache, setup.table)
     with pytest.raises(civic.CivicError):
         civic.civic_read_kv_quant(setup.cache, setup.table, start, x, x)
+
+
+def test_pinned_queries_and_rows():
+    """Pinned tensors may stand for device ones; what the call allocates is on the cache's device all the same."""
+    setup = Setup([20, 33], 2, 128, 4, 16, torch.bfloat16, seed=19)
+    q = setup.queries(2, 4)
+    want, want_lse = civic.civic_quant_attention(q.to(DEV), setup.cache, 0, setup.table, setup.lens, want_lse=True)
+    out, lse = civic.civic_quant_attention(q.pin_memory(), setup.cache, 0, setup.table, setup.lens, want_lse=True)
+    assert out.device == lse.device == torch.device(DEV)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    own = torch.empty_like(q).pin_memory()
+    out, lse = civic.civic_quant_attention(q.pin_memory(), setup.cache, 0, setup.table, setup.lens, want_lse=True, out=own)
+    torch.cuda.synchronize()
+    assert out is own and lse.device == torch.device(DEV)
+    assert torch.equal(own, want.cpu()) and torch.equal(lse, want_lse)
+    for kw in (dict(out=torch.empty_like(q)), dict(lse=torch.empty((2, 2, 4)))):
+        with pytest.raises(ValueError):
+            civic.civic_quant_attention(q.to(DEV), setup.cache, 0, setup.table, setup.lens, **kw)
+    # one pinned layer does not vouch for the next
+    cache = civic.quant_cache(2, 4, 2, 128, 16, 4, torch.bfloat16, DEV)
+    start, table = torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros((1, 1), dtype=torch.int32, device=DEV)
+    x = torch.randn(1, 4, 2, 128).bfloat16()
+    for rows in ([x.pin_memory(), x], [x.pin_memory(), x.to(DEV)], [x, x.pin_memory()]):
+        with pytest.raises(ValueError):
+            civic.civic_append_kv_quant(rows, [x.to(DEV)] * 2, start, cache, table)
+        with pytest.raises(ValueError):
+            civic.civic_append_kv_quant([x.to(DEV)] * 2, rows, start, cache, table)
+    pinned = x.pin_memory()
+    got = []
+    for rows in ([pinned, pinned], [x.to(DEV)] * 2):
+        cache.buffer.fill_(0)
+        civic.civic_append_kv_quant(rows, rows, start, cache, table)
+        got.append(cache.buffer.clone())
+    assert torch.equal(*got)
+
+
+def test_k_and_v_may_have_layer_strides_of_their_own():
+    cache = civic.quant_cache(2, 4, 2, 128, 16, 4, torch.bfloat16, DEV)
+    start, table = torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros((1, 1), dtype=torch.int32, device=DEV)
+    k = torch.randn(2, 1, 4, 2, 128, device=DEV).bfloat16()
+    v = torch.randn(4, 1, 4, 2, 128, device=DEV).bfloat16()
+    got = []
+    for other in (v[::2], v[::2].contiguous()):
+        cache.buffer.fill_(0)
+        civic.civic_append_kv_quant(k, other, start, cache, table)
+        got.append(cache.buffer.clone())
+    assert torch.equal(*got)
+    with pytest.raises(ValueError):
+        civic.civic_append_kv_quant(k, v[:2, :, ::2].repeat(1, 1, 2, 1, 1)[:, :, ::2], start, cache, table)
