@@ -899,6 +899,17 @@ def _same_rows(cache: QuantCache, first, x, what: str):
     return table
 
 
+def _new(shape, dtype: torch.dtype, device: torch.device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """Memory for a call on `stream`.  It comes from that stream's pool: memory of the current stream's may still
+    be in use there.  The caller reads it on the current stream, so neither stream reuses it too early."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        x = torch.empty(shape, dtype=dtype, device=device)
+    x.record_stream(torch.cuda.current_stream(device))
+    return x
+
+
 def _need_device(cache: QuantCache, x: torch.Tensor, what: str) -> None:
     """Raises unless x, which is not on the cache's device, is pinned host memory."""
     if x.device != cache.device and not x.is_pinned():
@@ -990,11 +1001,10 @@ def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_
     n_tok = _seq_words(cache, lens, n_seq, "lens")
     n_q = _seq_words(cache, q_lens, n_seq, "q_lens")
     max_pages = block_table.shape[1]
-    made = []  # allocated here: not to be handed out again before `stream` is done with it
     if out is None:
         # empty_like is the quicker of the two; pinned queries have it make pageable memory
-        out = torch.empty_like(q) if q.device == dev and q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=dev)
-        made.append(out)
+        out = (torch.empty_like(q) if stream is None and q.device == dev and q.is_contiguous()
+               else _new(q.shape, q.dtype, dev, stream))
         out_ptr = out.data_ptr()
     else:
         if out.shape != q.shape:
@@ -1010,23 +1020,18 @@ def civic_quant_attention(q: torch.Tensor, cache: QuantCache, layer: int, block_
             _need_device(cache, lse, "lse")
         lse_ptr = _dev_ptr(lse, "lse", torch.float32)
     elif want_lse:
-        lse = torch.empty((n_seq, q_len, q_heads), dtype=torch.float32, device=dev)
-        made.append(lse)
+        lse = _new((n_seq, q_len, q_heads), torch.float32, dev, stream)
         lse_ptr = lse.data_ptr()
     ws_ptr, ws_bytes = None, 0
     if workspace is None:
         ws_bytes = load().civic_quant_attention_workspace_bytes(cache.desc_ref, max_pages, n_seq, q_len, q_heads)
         if ws_bytes:
-            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
-            made.append(workspace)
+            workspace = _new(ws_bytes, torch.uint8, dev, stream)
             ws_ptr = workspace.data_ptr()
     else:
         if workspace.device != dev:
             _need_device(cache, workspace, "workspace")
         ws_ptr, ws_bytes = _dev_ptr(workspace, "workspace", torch.uint8), workspace.numel()
-    if stream is not None:
-        for t in made:
-            t.record_stream(stream)
     _call(cache, "civic_quant_attention", q.data_ptr(), _row_strides(seq, token, head), cache.ptr + layer * cache.layer_bytes,
           cache.desc_ref, table, max_pages, n_tok, n_q, n_seq, q_len, q_heads, dim ** -0.5 if scale is None else scale, causal,
           out_ptr, lse_ptr, ws_ptr, ws_bytes, stream=stream)

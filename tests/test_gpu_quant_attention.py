@@ -672,3 +672,21 @@ def test_k_and_v_may_have_layer_strides_of_their_own():
     assert torch.equal(*got)
     with pytest.raises(ValueError):
         civic.civic_append_kv_quant(k, v[:2, :, ::2].repeat(1, 1, 2, 1, 1)[:, :, ::2], start, cache, table)
+
+
+@pytest.mark.parametrize("pages", [4, 80])
+def test_results_on_another_stream_do_not_take_memory_that_the_current_one_still_writes(pages):
+    setup = Setup([20, 33], 2, 128, 4, 16, torch.bfloat16, seed=33, spare=pages)
+    q = setup.queries(40, 4).to(DEV)  # results of 80 KB
+    want, want_lse = civic.civic_quant_attention(q, setup.cache, 0, setup.table, setup.lens, want_lse=True)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    olds = [torch.empty_like(q) for _ in range(8)] + [torch.empty_like(want_lse) for _ in range(8)]
+    torch.cuda._sleep(20_000_000)
+    for old in olds:
+        old.fill_(7.0)
+    del olds, old
+    out, lse = civic.civic_quant_attention(q, setup.cache, 0, setup.table, setup.lens, want_lse=True, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
