@@ -532,7 +532,7 @@ civic_status_t civic_append_kv_quant(const void* const* k_new, const void* const
 
 /*
  * civic_read_kv_quant -- rows of the quantised cache as dense tensors, s * code + m rounded to the
- * payload type.  Paper: no counterpart.
+ * payload type (next to the end of its range to its largest number, not to infinity).  Paper: no counterpart.
  *
  * Token start[s] + j (start NULL: j) of sequence s becomes row j < counts[s] of k_dst[l] / v_dst[l];
  * the rows from counts[s] on are left as they were.

@@ -650,7 +650,8 @@ __device__ __forceinline__ void qa_store(const QuantAttnParams& p, int seq, int 
     const int token = row / p.group, h = head * p.group + row - token * p.group;
     const size_t at = ((size_t)seq * p.q_len + token) * p.q_heads + h;
     const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that sees nothing: zeros
-    const uint2 v = make_uint2(Half16<T>::pack(o.x * inv, o.y * inv), Half16<T>::pack(o.z * inv, o.w * inv));
+    // V's values may lie a little beyond T's largest number (values8)
+    const uint2 v = make_uint2(Half16<T>::pack_finite(o.x * inv, o.y * inv), Half16<T>::pack_finite(o.z * inv, o.w * inv));
     *reinterpret_cast<uint2*>(p.out + (at * hd + channel) * 2) = v;
     if (channel == 0 && p.lse) p.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }

@@ -108,6 +108,13 @@ struct Half16<__nv_bfloat16> {
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
         return d;
     }
+    // The type's largest number instead of an infinity; NaN stays NaN.
+    __device__ static uint32_t pack_finite(float lo, float hi)
+    {
+        uint32_t d;
+        asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+        return d;
+    }
     // The least bf16 whose `top`-fold is not below range (0 where that has no normal reciprocal), from
     // q = range / top or slightly less: cut to bf16 it is that number or the one below it, which the
     // exact product top * s (8 + 8 bits) tells apart.
@@ -139,6 +146,12 @@ struct Half16<__half> {
     {
         uint32_t d;
         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+        return d;
+    }
+    __device__ static uint32_t pack_finite(float lo, float hi)
+    {
+        uint32_t d;
+        asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
         return d;
     }
     __device__ static uint32_t scale_bits(float range, float q, float top)
@@ -205,12 +218,15 @@ __device__ __forceinline__ Codes16 quantise16(const Row16& v)
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
     inv = s > 0.f ? __uint_as_float(__float_as_uint(inv) + 1u) : 0.f;
-    const float base = low - 0.5f * s;  // the 1/2 of the rounding
+    // near the end of fp32 (bf16 only) everything by half, so that x - base stays finite: it is at most range + s / 2
+    const float h = std::is_same<T, __nv_bfloat16>::value && range > 0x1p124f ? 0.5f : 1.f;
+    const float base = fmaf(low, h, -0.5f * h * s);  // the 1/2 of the rounding
+    if (h != 1.f) inv *= 2.f;
     uint32_t c[16];  // code in the low byte
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const float x = (i & 1) ? H::hi(v.x[i >> 1]) : H::lo(v.x[i >> 1]);
-        c[i] = __float_as_uint(__fmaf_rd(x - base, inv, 8388608.f));  // floor in the low bits
+        c[i] = __float_as_uint(__fmaf_rd(fmaf(x, h, -base), inv, 8388608.f));  // floor in the low bits
     }
     if constexpr (BITS == 4) {
 #pragma unroll
@@ -228,7 +244,8 @@ __device__ __forceinline__ Codes16 quantise16(const Row16& v)
     return r;
 }
 
-// The values of 8 codes, rounded to T.
+// The values of 8 codes, rounded to T.  s is rounded up, so that the largest code may stand for a little more than
+// the group's maximum: next to the end of T's range that is no reason for an infinity.
 template <typename T, int BITS>
 __device__ __forceinline__ uint4 values8(const Codes8& c)
 {
@@ -240,8 +257,8 @@ __device__ __forceinline__ uint4 values8(const Codes8& c)
         const float code = __uint_as_float((w & (BITS == 4 ? 15u : 255u)) | 0x4B000000u) - 8388608.f;
         return fmaf(s, code, m);
     };
-    return make_uint4(H::pack(value(0), value(1)), H::pack(value(2), value(3)), H::pack(value(4), value(5)),
-                      H::pack(value(6), value(7)));
+    return make_uint4(H::pack_finite(value(0), value(1)), H::pack_finite(value(2), value(3)), H::pack_finite(value(4), value(5)),
+                      H::pack_finite(value(6), value(7)));
 }
 
 // ---- the kernels -----------------------------------------------------------------------------------

@@ -690,3 +690,39 @@ def test_results_on_another_stream_do_not_take_memory_that_the_current_one_still
     out, lse = civic.civic_quant_attention(q, setup.cache, 0, setup.table, setup.lens, want_lse=True, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_values_at_the_end_of_fp16_stay_finite(bits):
+    """A rounded-up scale may put a group's largest value a little beyond 65504."""
+    big = torch.finfo(torch.float16).max
+
+    def edit(k, v):
+        v[..., ::2], v[..., 1::2] = big, -big
+
+    setup = Setup([20, 700], 1, 128, bits, 16, torch.float16, seed=34, edit=edit)
+    q = setup.queries(3, 2)
+    out, lse = attend(setup, q)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    # off by at most half a step, the weights' and sums' roundings (2^-11 and less of 65504) and the last rounding
+    step = 2 * big / (15 if bits == 4 else 255) * (1 + 2.0**-10)
+    want = torch.tensor([big, -big], dtype=torch.float64).repeat(64)
+    assert float((out.double() - want).abs().max()) <= step / 2 + big * 2.0**-10
+
+
+@pytest.mark.parametrize("q_len", [3, 300])
+def test_a_query_that_is_not_finite_spoils_its_row_only(q_len):
+    setup = Setup([900, 400], 2, 128, 4, 16, torch.bfloat16, seed=35)
+    q = setup.queries(q_len, 8).to(DEV)
+    assert takes_tcgen05(setup, q) == (q_len == 300)
+    want, want_lse = attend(setup, q, causal=False)
+    bad = q.clone()
+    bad[0, 1, 3, 7], bad[1, 2, 0, 0], bad[1, 0, 5, 127] = float("nan"), float("inf"), float("-inf")
+    got, lse = attend(setup, bad, causal=False)
+    spoilt = torch.zeros(2, q_len, 8, dtype=torch.bool)
+    spoilt[0, 1, 3] = spoilt[1, 2, 0] = spoilt[1, 0, 5] = True
+    assert bool(torch.isnan(got[spoilt]).all()) and bool(torch.isnan(lse[spoilt]).all())
+    assert bool(torch.isfinite(got).all(-1)[~spoilt].all())
+    # weights of the other rows may be taken relative to another reference: a rounding of each weight (fp16) and of the result
+    assert float((got[~spoilt].double() - want[~spoilt].double()).abs().max()) <= (2.0**-10 + 2.0**-8) * 8
+    assert float((lse[~spoilt] - want_lse[~spoilt]).abs().max()) <= 1e-5
