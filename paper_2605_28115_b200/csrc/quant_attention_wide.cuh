@@ -26,7 +26,7 @@
 // fp16's range is kept by powers of two: per query row, and per tile of 16 tokens for K (the largest
 // s of a tile is in [2^-9, 2^-8)) and V (the largest |v| in [2^-7, 2^-6)): then a code enters the
 // multiply-add as the fp16 subnormal that its bits are (code * 2^-24, s * 2^24 below 2^16), one instruction
-// for two values.  Where a tile's tokens differ by more than 2^5 (K) or 2^8 (V) in size every token has a
+// for two values.  Where a tile's tokens differ by more than 2^5 in size every token has a
 // power of its own (the softmax then looks at every column's factors).
 // fp16 results have 11 bits themselves: for them quant_attention.cuh, which loses none of V's, is used.
 //
@@ -178,8 +178,10 @@ struct QwVStage {                    // beside a V' stage
 };
 struct QwSync {
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full;
-    uint64_t s_full[2][2], p_ready[2][2];  // [tile of rows][half of the block]
-    uint64_t pv_done[2], drained;          // products with V issued so far are complete
+    // [tile of rows][half of the block], a phase for each block.  A parity tells the current phase from the one before
+    // only: who waits for pv_done must know the phase before to be complete, and its own not to be overtaken.
+    uint64_t s_full[2][2], p_ready[2][2], pv_done[2][2];
+    uint64_t drained;
     float row_factor[2][kQwRows];    // per item (alternating) and row: takes raw scores to base-2 logits
     QwKStage k_stage[4];
     QwVStage v_stage[2];
@@ -285,7 +287,7 @@ __device__ __forceinline__ int qw_params_v(const uint32_t (&from)[HD / 64], uint
     float most = mag;
 #pragma unroll
     for (int d = 2; d < 32; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
-    const bool uneven = __any_sync(0xFFFFFFFFu, mag > 0.f && mag < most * 0x1p-8f);
+    const bool uneven = __any_sync(0xFFFFFFFFu, mag > 0.f && mag < most * 0x1p-5f);
     const bool other_bad = __shfl_xor_sync(0xFFFFFFFFu, (int)bad, 1) != 0;  // every lane takes part
     bad = bad || other_bad;
     nan = clear_nan && bad;
@@ -366,8 +368,8 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
             for (int h = 0; h < 2; ++h) {
                 mbar_init(&sy.s_full[i][h], 1);
                 mbar_init(&sy.p_ready[i][h], 4);
+                mbar_init(&sy.pv_done[i][h], 1);
             }
-            mbar_init(&sy.pv_done[i], 1);
         }
         mbar_init(&sy.q_full, kQwProducers);
         mbar_init(&sy.drained, 1);
@@ -689,7 +691,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
 #pragma unroll
                         for (int kk = 0; kk < kQwBlock / 32; ++kk)
                             umma_bf16_a_tmem(d, a + 8u * kk, desc(hi_v, b0 + 128u * kk), idesc_o, kk != 0 ? 1u : keep);
-                        umma_commit(&sy.pv_done[t]);
+                        umma_commit(&sy.pv_done[t][h]);
                     }
                     __syncwarp();
                     if (more) {
@@ -788,6 +790,7 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
 #pragma unroll
                         for (int i = 0; i < 32; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) - up);
                         const uint32_t f2 = pack_half2(f, f);
+                        if ((c0 & 63) != 0) tmem_store_wait();  // this warp's P, before it is read again
 #pragma unroll 1
                         for (int q = 0; q < (c0 & 63) / 2; q += 8) {
                             uint32_t w[8];
@@ -798,8 +801,8 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
                         }
                         // O is complete up to the previous half once its products are (those of the half before that
                         // were when this half's scores came)
-                        const int halves = 2 * turn + (c0 >> 6);
-                        if (b > 0 || c0 >= 64) ok = ok && wait(&sy.pv_done[t], (halves - 1) & 1, kAggTimeoutAcc);
+                        if (c0 >= 64) ok = ok && wait(&sy.pv_done[t][0], turn & 1, kAggTimeoutAcc);
+                        else if (b > 0) ok = ok && wait(&sy.pv_done[t][1], (turn - 1) & 1, kAggTimeoutAcc);
                         tc_fence_after_sync();
 #pragma unroll 1
                         for (int q = 0; (b > 0 || c0 >= 64) && q < HD; q += 8) {
@@ -862,9 +865,9 @@ __global__ void __launch_bounds__(kQwThreads, 1) quant_attention_wide_kernel(con
             }
             if (!ok) break;
             // ---- the item's rows, or this block's part of them
-            // both halves of the last block, in order: a barrier two phases behind looks like one that is up to date
-            if (!(ok = wait(&sy.pv_done[t], (2 * turn - 2) & 1, kAggTimeoutAcc))) break;
-            if (!(ok = wait(&sy.pv_done[t], (2 * turn - 1) & 1, kAggTimeoutAcc))) break;
+            // the second half of the last block, and with it all products before (that of the block before was complete
+            // when this block's scores came, or at the end of the last item)
+            if (!(ok = wait(&sy.pv_done[t][1], (turn - 1) & 1, kAggTimeoutAcc))) break;
             tc_fence_after_sync();
             const bool whole = it.block == 0 && n_blocks == it.units;
             float* slot = p.partial + (size_t)(2 * blockIdx.x + (it.block > 0 ? 0 : 1)) * qw_slot_floats(HD);
