@@ -11,8 +11,8 @@
 //   softmax    maximum, exp2, P_t packed over S_t; O_t is rescaled only when a row's reference moved
 // Scores, weights and products go by halves of a block (64 tokens): while the softmax works on one half the
 // tensor cores multiply the other half's weights and make the next scores, so that neither waits for the
-// other's latency.  500 query tokens, 32 heads of 128, on 4 sequences of 4001 in 4 bits (123 GFLOP): 216 us =
-// 570 TFLOP/s, a third of the tensor cores' measured rate; softmax, MMA issue and producers are each busy for 70
+// other's latency.  500 query tokens, 32 heads of 128, on 4 sequences of 4001 in 4 bits (123 GFLOP): 221 us =
+// 557 TFLOP/s, a third of the tensor cores' measured rate; softmax, MMA issue and producers are each busy for 70
 // to 85 % of the 6700 cycles that a unit of 256 rows x 128 tokens takes.
 //
 // fp16 operands, and scores without a rounding in them.  In the middle of its codes a group is
